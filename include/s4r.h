@@ -393,6 +393,115 @@ s4r_status s4r_dense_decode(const s4r_config* cfg, int64_t N, const void* q, con
                             hipStream_t stream);
 
 /*
+ * Norms of the query and key heads and the position rotation in one pass, for
+ * layers that normalise them (Qwen3's) and for the rows of a full KV cache.  Per
+ * head of each token:  y = x / sqrt(mean(x^2) + eps) * weight, then, unless
+ * cfg.rope_theta is 0, dims (i, i + d_h / 2) turned by
+ * positions[token] * theta^(-2 i / d_h).  A NULL weight leaves that side's heads
+ * unnormalised.  Without the rotation the outputs are the pre-RoPE rows that
+ * the compressed path takes (s4r_prefill_bases, s4r_prefill_project,
+ * s4r_project_append, s4r_decode_step); with it they are the query of
+ * s4r_kv8_decode and the key rows of s4r_kv8_write.
+ *   q [n_tokens, h_q, d_h], k [n_tokens, h_kv, d_h] in the storage dtype, the heads
+ *   of a token packed, tokens q_stride / k_stride elements apart (rows of a
+ *   fused projection; a multiple of 16 bytes, at least the heads' width).
+ *   Either may be NULL with its output: the other side alone.
+ *   q_out, k_out: as q, k with strides q_out_stride, k_out_stride.  An output
+ *   may be its own input (same pointer and stride); any other overlap of an
+ *   output's rows with a tensor of the call is an error of the caller.
+ *   q_weight, k_weight [d_h] storage dtype or NULL; eps finite and >= 0.
+ *   positions int32 [n_tokens], 4-byte aligned, any values (NULL only when
+ *   rope_theta is 0).
+ * Sums of squares are fp64, everything else fp32, rounded once.  Uses cfg's head
+ * counts, head_dim, rope_theta and dtype.
+ */
+s4r_status s4r_qk_norm_rope(const s4r_config* cfg, int64_t n_tokens, const void* q, int64_t q_stride,
+                            const void* k, int64_t k_stride, const void* q_weight, const void* k_weight,
+                            float eps, const int32_t* positions, void* q_out, int64_t q_out_stride,
+                            void* k_out, int64_t k_out_stride, hipStream_t stream);
+
+/*
+ * Full KV cache in 8 bits.  Tokens are held in blocks of 64; each block of one
+ * (sequence, KV head) has one fp32 scale per side, and a token's value is
+ * code * scale.  With T = ceil(capacity / 64) blocks per sequence and KV head:
+ *   k_codes, v_codes  [B, h_kv, T, 64 * d_h] bytes   (s4r_kv8_size: code_bytes each)
+ *   k_scales, v_scales [B, h_kv, T] fp32             (scale_count each)
+ * and in a block, element (t, d) at
+ *   keys    (t/16)*16*d_h + (d/64)*1024 + ((d%64)/16)*256 + (t%16)*16 + d%16
+ *   values  (d/16)*1024 + ((t%16)/4)*256 + (d%16)*16 + (t%4)*4 + t/16
+ * (the order in which the attention kernel's matrix operands take them).
+ * Formats: S4R_KV_INT8 (codes -127..127, scale = amax / 127 rounded to fp32) and
+ * S4R_KV_E4M3 (OCP e4m3 codes, scale = the smallest power of two with
+ * amax <= 448 * scale), amax the largest |value| written; codes are the nearest,
+ * ties to even, of value / scale, exactly.  A block whose amax is below 2^-90
+ * gets scale 0 and zero codes.  A NaN or infinity among a block's values gives
+ * it a NaN scale: the whole block reads as NaN, and so does the attention of the heads
+ * that see it, until the block is written again from its first token.
+ */
+enum { S4R_KV_INT8 = 0, S4R_KV_E4M3 = 1 };
+#define S4R_KV8_BLOCK 64
+typedef struct {
+  int32_t format;        /* S4R_KV_INT8 | S4R_KV_E4M3 */
+  void* k_codes;
+  float* k_scales;
+  void* v_codes;
+  float* v_scales;
+} s4r_kv8;
+
+s4r_status s4r_kv8_size(const s4r_config* cfg, size_t* code_bytes, size_t* scale_count);
+
+/*
+ * Rows into the cache, quantised as they are written.  k_rows, v_rows: B * n_rows
+ * rows of h_kv * d_h elements in the storage dtype, row b * n_rows + i being
+ * sequence b's i-th, k_stride / v_stride elements apart (a multiple of 16 bytes,
+ * at least the width).  Row i of sequence b becomes token first_b + i,
+ * first_b = starts[b] (int32 [B] on the device, 4-byte aligned) or row0 where
+ * starts is NULL, for i < counts[b] (device, clamped to [0, n_rows]; NULL: all).
+ * A sequence whose range does not lie in [0, capacity) is left as it is.
+ *   A call that starts inside a block keeps the block's earlier tokens: the scale
+ * becomes the larger of the present one and the new rows' own, and where it grows
+ * the earlier tokens are written anew from the values they stood for.  A call
+ * that starts at a block's first token sets the scale afresh.  The earlier tokens
+ * must have been written, or the cache have been zeros.  Tokens of a block
+ * behind the last one written keep their codes (their scale may have changed: a
+ * sequence holds the tokens up to the last one written).
+ * 1 <= n_rows <= capacity.
+ */
+s4r_status s4r_kv8_write(const s4r_config* cfg, const s4r_kv8* cache, int64_t n_rows, int64_t row0,
+                         const int32_t* starts, const int32_t* counts, const void* k_rows,
+                         int64_t k_stride, const void* v_rows, int64_t v_stride, hipStream_t stream);
+
+/*
+ * Rows out of the cache: k_out, v_out [B, n_rows, h_kv * d_h] in the storage
+ * dtype (code * scale in fp32, rounded once), row i of sequence b the token
+ * first_b + i as above; rows from counts[b] on are zeros, and so are all rows
+ * of a sequence whose range does not lie in [0, capacity).
+ */
+s4r_status s4r_kv8_read(const s4r_config* cfg, const s4r_kv8* cache, int64_t n_rows, int64_t row0,
+                        const int32_t* starts, const int32_t* counts, void* k_out, void* v_out,
+                        hipStream_t stream);
+
+/*
+ * Attention of each sequence's newest n_q query tokens over the 8-bit cache:
+ * query token i of n_q sees the tokens 0 .. N_b - n_q + i of sequence b,
+ *   out[b, i, h] = softmax(q_h K_j^T / sqrt(d_h)) V_j,  j = h / G,
+ * with the cache as it is held (keys rotated by whoever wrote them) and q
+ * [B, n_q, h_q, d_h] in the storage dtype rotated alike (s4r_qk_norm_rope;
+ * rope_theta is not used).  out fp32 [B, n_q, h_q, d_h].  N_b = lengths[b] (int32
+ * [B] on the device, 4-byte aligned, clamped to [0, N]) or N where lengths is NULL;
+ * the work follows the lengths on the device, so a captured graph may be replayed
+ * as sequences grow up to N.  A query token that sees nothing gets zeros.  Query
+ * elements must be finite.  1 <= N <= capacity, 1 <= n_q and n_q * G <= 128.
+ * ws: s4r_kv8_workspace_size bytes, 256-byte aligned; its contents do not matter.
+ * Scores and sums are fp32; the 8-bit codes and bf16 queries enter the matrix cores
+ * exactly, the weights (and fp32 queries) as three bf16 parts, 24 bits.
+ */
+s4r_status s4r_kv8_workspace_size(const s4r_config* cfg, int32_t n_q, size_t* bytes);
+s4r_status s4r_kv8_decode(const s4r_config* cfg, const s4r_kv8* cache, int64_t N, const int32_t* lengths,
+                          int32_t n_q, const void* q, float* out, void* ws, size_t ws_bytes,
+                          hipStream_t stream);
+
+/*
  * Compressed cache update alone (Section 3.2.1): c^K = k_new B^K and
  * c^V = v_new B^V, rounded to the storage dtype (fp64 accumulation, then
  * fp32 and bf16 round-to-nearest-even), written into coefficient row `row`.

@@ -12,6 +12,8 @@ from ._lib import Config, S4RError  # noqa: F401
 _lib.load()
 
 from .api import (  # noqa: E402,F401
+    KV8Cache,
+    alloc_kv8_workspace,
     alloc_window_state,
     alloc_workspace,
     decode_step,
@@ -20,6 +22,12 @@ from .api import (  # noqa: E402,F401
     decode_step_windowed,
     dense_decode,
     full_recon_decode,
+    kv8_alloc,
+    kv8_decode,
+    kv8_read,
+    kv8_size,
+    kv8_workspace_size,
+    kv8_write,
     make_config,
     num_selected,
     pack_coef,
@@ -30,6 +38,7 @@ from .api import (  # noqa: E402,F401
     prefill_project,
     project_append,
     project_queries,
+    qk_norm_rope,
     rank_stride,
     read_bandwidth,
     reconstruct,

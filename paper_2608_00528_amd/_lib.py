@@ -13,6 +13,8 @@ STATUS_NAMES = {0: "OK", 1: "NULL_ARG", 2: "BAD_SHAPE", 3: "UNSUPPORTED", 4: "WO
 S4R_FP32, S4R_BF16 = 0, 1
 S4R_POOL_MAX, S4R_POOL_AVG = 0, 1
 S4R_AGG_MEAN, S4R_AGG_MAX = 0, 1
+S4R_KV_INT8, S4R_KV_E4M3 = 0, 1
+KV8_BLOCK = 64
 
 EXPORTS = (
     "s4r_workspace_size", "s4r_num_selected", "s4r_last_error", "s4r_version",
@@ -23,6 +25,7 @@ EXPORTS = (
     "s4r_full_recon_decode", "s4r_prefill_num_samples", "s4r_prefill_bases_workspace_size", "s4r_prefill_bases",
     "s4r_project_queries", "s4r_decode_step_noalloc",
     "s4r_window_state_size", "s4r_window_state_init", "s4r_decode_step_windowed",
+    "s4r_qk_norm_rope", "s4r_kv8_size", "s4r_kv8_write", "s4r_kv8_read", "s4r_kv8_workspace_size", "s4r_kv8_decode",
 )
 
 
@@ -49,11 +52,22 @@ class Config(ctypes.Structure):
     ]
 
 
+class KV8(ctypes.Structure):
+    _fields_ = [
+        ("format", ctypes.c_int32),
+        ("k_codes", ctypes.c_void_p),
+        ("k_scales", ctypes.c_void_p),
+        ("v_codes", ctypes.c_void_p),
+        ("v_scales", ctypes.c_void_p),
+    ]
+
+
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
 _CFG = ctypes.POINTER(Config)
+_KV8 = ctypes.POINTER(KV8)
 
 _SIGS = {
     "s4r_workspace_size": (_I32, [_CFG, ctypes.POINTER(_SZ)]),
@@ -88,6 +102,12 @@ _SIGS = {
     "s4r_window_state_init": (_I32, [_CFG, _I64, _P, _P, _P, _P, _SZ, _P]),
     "s4r_decode_step_windowed": (_I32, [_CFG, _I64, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P, _P,
                                         _P, _SZ, _P]),
+    "s4r_qk_norm_rope": (_I32, [_CFG, _I64, _P, _I64, _P, _I64, _P, _P, ctypes.c_float, _P, _P, _I64, _P, _I64, _P]),
+    "s4r_kv8_size": (_I32, [_CFG, ctypes.POINTER(_SZ), ctypes.POINTER(_SZ)]),
+    "s4r_kv8_write": (_I32, [_CFG, _KV8, _I64, _I64, _P, _P, _P, _I64, _P, _I64, _P]),
+    "s4r_kv8_read": (_I32, [_CFG, _KV8, _I64, _I64, _P, _P, _P, _P, _P]),
+    "s4r_kv8_workspace_size": (_I32, [_CFG, _I32, ctypes.POINTER(_SZ)]),
+    "s4r_kv8_decode": (_I32, [_CFG, _KV8, _I64, _P, _I32, _P, _P, _P, _SZ, _P]),
 }
 
 _lib = None

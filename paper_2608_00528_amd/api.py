@@ -15,6 +15,7 @@ from . import _lib as L
 _DTYPES = {"bf16": (L.S4R_BF16, torch.bfloat16), "fp32": (L.S4R_FP32, torch.float32)}
 _POOL = {"max": L.S4R_POOL_MAX, "avg": L.S4R_POOL_AVG}
 _AGG = {"mean": L.S4R_AGG_MEAN, "max": L.S4R_AGG_MAX}
+_KV_FORMATS = {"int8": L.S4R_KV_INT8, "e4m3": L.S4R_KV_E4M3}
 
 
 def make_config(*, batch, n_q_heads, n_kv_heads, head_dim, rank, capacity, basis_groups=1, n_sink=4,
@@ -399,6 +400,241 @@ def dense_decode(cfg, n_tokens, q, k_cache, v_cache, ws, out=None):
     L.check(L.load().s4r_dense_decode(_cfgp(cfg), n_tokens, _ptr(q, "q", dt), _ptr(k_cache, "k_cache", dt),
                                       _ptr(v_cache, "v_cache", dt), _ptr(out, "out", torch.float32),
                                       _ptr(ws, "ws", torch.uint8), ws.numel(), _stream()))
+    return out
+
+
+def _here(t, name):
+    """The tensor's device has to be the current one: the launch goes to its stream."""
+    if t is not None and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, not on the current device {torch.cuda.current_device()}")
+
+
+def _rows(t, name, dtype, width):
+    """(address, rows, elements between rows) of a GPU tensor [..., heads, head_dim] or [..., width] whose last
+    axes are packed to rows of `width` and whose leading axes step evenly from row to row."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    _here(t, name)
+    shape, strides = t.shape, t.stride()
+    d, n = len(shape), 1
+    while d and n < width:
+        d -= 1
+        if strides[d] != n and shape[d] != 1:
+            raise ValueError(f"{name}: the elements of a row must be packed")
+        n *= shape[d]
+    if n != width:
+        raise ValueError(f"{name} has shape {tuple(shape)}: rows of {width} elements were expected")
+    rows, stride = 1, None
+    for i in range(d - 1, -1, -1):
+        if shape[i] != 1:
+            if stride is None:
+                stride = strides[i]
+            elif strides[i] != rows * stride:
+                raise ValueError(f"{name}: the rows must be evenly spaced")
+            rows *= shape[i]
+    if rows == 0:
+        raise ValueError(f"{name} has no rows")
+    return t.data_ptr(), rows, width if stride is None else stride
+
+
+def _ints(t, name, n):
+    if t is None:
+        return None
+    p = _ptr(t, name, torch.int32)
+    _here(t, name)
+    if t.numel() != n:
+        raise ValueError(f"{name} has {t.numel()} entries, expected {n}")
+    return p
+
+
+def qk_norm_rope(cfg, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, q_out=None, k_out=None):
+    """Query heads q [..., h_q, d_h] and key heads k [..., h_kv, d_h] of the same tokens, each head normalised
+    (x / sqrt(mean(x^2) + eps) * weight [d_h]; not where its weight is None) and rotated by its token's position
+    (int32, one per token; rope_theta = 0: not rotated, positions may be None).  q or k may be None.  The tokens may
+    be slices of a fused projection's rows; outputs (new packed tensors by default) may be the inputs themselves.
+    Returns (q_out, k_out)."""
+    dt = storage_dtype(cfg)
+    dh, n = cfg.head_dim, None
+    args, outs = [], []
+    for name, x, o, heads in (("q", q, q_out, cfg.n_q_heads), ("k", k, k_out, cfg.n_kv_heads)):
+        if x is None:
+            if o is not None:
+                raise ValueError(f"{name}_out without {name}")
+            args += [None, 0, None, 0]
+            outs.append(None)
+            continue
+        p, rows, stride = _rows(x, name, dt, heads * dh)
+        if n is not None and rows != n:
+            raise ValueError(f"q has {n} tokens and k {rows}")
+        n = rows
+        if o is None:
+            o = torch.empty(x.shape, dtype=dt, device=x.device)
+        po, ro, so = _rows(o, name + "_out", dt, heads * dh)
+        if ro != n:
+            raise ValueError(f"{name}_out has {ro} tokens, expected {n}")
+        args += [p, stride, po, so]
+        outs.append(o)
+    if n is None:
+        raise ValueError("q or k is required")
+    _apart(args, n, cfg, dt)
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _here(w, name)
+            if w.numel() != dh:
+                raise ValueError(f"{name} has {w.numel()} entries, expected {dh}")
+    L.check(L.load().s4r_qk_norm_rope(
+        _cfgp(cfg), n, args[0], args[1], args[4], args[5], _ptr(q_weight, "q_weight", dt, False),
+        _ptr(k_weight, "k_weight", dt, False), eps, _ints(positions, "positions", n), args[2], args[3], args[6],
+        args[7], _stream()))
+    return tuple(outs)
+
+
+def _apart(args, n, cfg, dt):
+    """An output's rows may be its own input's, and otherwise no other rows of the call.  Rows of one fused
+    buffer (equal strides) interleave without overlapping."""
+    es = 2 if dt == torch.bfloat16 else 4
+    dh = cfg.head_dim
+    wq, wk = cfg.n_q_heads * dh * es, cfg.n_kv_heads * dh * es
+    q, k = (args[0], args[1] * es, wq), (args[4], args[5] * es, wk)
+    qo, ko = (args[2], args[3] * es, wq), (args[6], args[7] * es, wk)
+
+    def overlap(a, b):
+        if a[0] is None or b[0] is None:
+            return False
+        if a[0] + (n - 1) * a[1] + a[2] <= b[0] or b[0] + (n - 1) * b[1] + b[2] <= a[0]:
+            return False
+        if a[1] != b[1] or n == 1:
+            return True
+        off = (b[0] - a[0]) % a[1]
+        return off < a[2] or off + b[2] > a[1]
+
+    for name, o, own, others in (("q_out", qo, q, (k,)), ("k_out", ko, k, (q,))):
+        if o[0] is None:
+            continue
+        if any(overlap(o, x) for x in others) or (o[:2] != own[:2] and overlap(o, own)):
+            raise ValueError(f"{name} overlaps an input of the call that is not its own")
+    if overlap(qo, ko):
+        raise ValueError("q_out and k_out overlap")
+
+
+class KV8Cache:
+    """The tensors of an 8-bit KV cache (kv8_alloc): codes [B, h_kv, T, 64 d_h] uint8 and scales [B, h_kv, T]
+    fp32 of both sides, T = ceil(capacity / 64); format "int8" or "e4m3"."""
+
+    __slots__ = ("format", "k_codes", "k_scales", "v_codes", "v_scales", "_c")
+
+    def __init__(self, format, k_codes, k_scales, v_codes, v_scales):
+        if format not in _KV_FORMATS:
+            raise ValueError(f"format {format!r}: one of {sorted(_KV_FORMATS)} was expected")
+        self.format = format
+        self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
+        self._c = L.KV8(_KV_FORMATS[format], _ptr(k_codes, "k_codes", torch.uint8),
+                        _ptr(k_scales, "k_scales", torch.float32), _ptr(v_codes, "v_codes", torch.uint8),
+                        _ptr(v_scales, "v_scales", torch.float32))
+
+
+def kv8_size(cfg):
+    """(bytes of codes, scales) of one side of the 8-bit cache."""
+    n, m = ctypes.c_size_t(), ctypes.c_size_t()
+    L.check(L.load().s4r_kv8_size(_cfgp(cfg), ctypes.byref(n), ctypes.byref(m)))
+    return n.value, m.value
+
+
+def kv8_alloc(cfg, format="int8", device="cuda"):
+    """An empty 8-bit cache of cfg.capacity tokens per sequence."""
+    if format not in _KV_FORMATS:
+        raise ValueError(f"format {format!r}: one of {sorted(_KV_FORMATS)} was expected")
+    kv8_size(cfg)                                    # the library's own checks of cfg
+    shape = (cfg.batch, cfg.n_kv_heads, (cfg.capacity + L.KV8_BLOCK - 1) // L.KV8_BLOCK)
+    sides = []
+    for _ in range(2):
+        sides += [torch.zeros(shape + (L.KV8_BLOCK * cfg.head_dim,), dtype=torch.uint8, device=device),
+                  torch.zeros(shape, dtype=torch.float32, device=device)]
+    return KV8Cache(format, *sides)
+
+
+def _kv8(cfg, cache):
+    """The C view of a cache, its tensors' sizes checked against cfg."""
+    if not isinstance(cache, KV8Cache):
+        raise ValueError("cache must be a KV8Cache")
+    blocks = cfg.batch * cfg.n_kv_heads * ((cfg.capacity + L.KV8_BLOCK - 1) // L.KV8_BLOCK)
+    for name, n in (("k_codes", blocks * L.KV8_BLOCK * cfg.head_dim), ("k_scales", blocks),
+                    ("v_codes", blocks * L.KV8_BLOCK * cfg.head_dim), ("v_scales", blocks)):
+        t = getattr(cache, name)
+        if t.numel() != n:
+            raise ValueError(f"{name} has {t.numel()} elements, expected {n}")
+        _here(t, name)
+    return ctypes.byref(cache._c)
+
+
+def kv8_write(cfg, cache, k, v, row0=0, starts=None, counts=None):
+    """Quantise rows k, v [B, n, h_kv d_h] (or [B, n, h_kv, d_h]; evenly spaced rows) into the cache as tokens
+    starts[b] + i (int32 GPU tensor; row0 + i without it) for i < counts[b] (all without it).  A sequence whose range
+    does not fit is left as it is."""
+    dt, width = storage_dtype(cfg), cfg.n_kv_heads * cfg.head_dim
+    c = _kv8(cfg, cache)
+    pk, rows, sk = _rows(k, "k", dt, width)
+    pv, rv, sv = _rows(v, "v", dt, width)
+    if rows != rv or rows % cfg.batch:
+        raise ValueError(f"k has {rows} rows and v {rv}: a multiple of the batch {cfg.batch}, the same for both, "
+                         "was expected")
+    L.check(L.load().s4r_kv8_write(_cfgp(cfg), c, rows // cfg.batch, row0, _ints(starts, "starts", cfg.batch),
+                                   _ints(counts, "counts", cfg.batch), pk, sk, pv, sv, _stream()))
+
+
+def kv8_read(cfg, cache, n_rows, row0=0, starts=None, counts=None, k=None, v=None):
+    """The tokens starts[b] + i (row0 + i), i < n_rows, of every sequence in the storage dtype: (k, v)
+    [B, n_rows, h_kv d_h].  Rows from counts[b] on are zeros."""
+    dt = storage_dtype(cfg)
+    c = _kv8(cfg, cache)
+    shape = (cfg.batch, n_rows, cfg.n_kv_heads * cfg.head_dim)
+    out = []
+    for name, t in (("k", k), ("v", v)):
+        if t is None:
+            t = torch.empty(shape, dtype=dt, device=cache.k_codes.device)
+        elif t.numel() != shape[0] * shape[1] * shape[2]:
+            raise ValueError(f"{name} has {t.numel()} elements, expected {shape}")
+        _here(t, name)
+        out.append(t)
+    L.check(L.load().s4r_kv8_read(_cfgp(cfg), c, n_rows, row0, _ints(starts, "starts", cfg.batch),
+                                  _ints(counts, "counts", cfg.batch), _ptr(out[0], "k", dt), _ptr(out[1], "v", dt),
+                                  _stream()))
+    return tuple(out)
+
+
+def kv8_workspace_size(cfg, n_queries=1):
+    n = ctypes.c_size_t()
+    L.check(L.load().s4r_kv8_workspace_size(_cfgp(cfg), n_queries, ctypes.byref(n)))
+    return n.value
+
+
+def alloc_kv8_workspace(cfg, n_queries=1, device="cuda"):
+    return torch.empty(kv8_workspace_size(cfg, n_queries), dtype=torch.uint8, device=device)
+
+
+def kv8_decode(cfg, cache, n_tokens, q, ws, lengths=None, out=None):
+    """Attention of the newest query tokens q [B, h_q, d_h] or [B, n, h_q, d_h] (rotated as the cached keys are)
+    over the 8-bit cache: tokens 0 .. n_tokens - 1 of every sequence, or of lengths[b] (int32 GPU tensor, at most
+    n_tokens are used).  Query token i of n sees all but the newest n - 1 - i tokens.  ws: alloc_kv8_workspace.
+    Returns fp32 of q's shape."""
+    dt = storage_dtype(cfg)
+    c = _kv8(cfg, cache)
+    per = cfg.batch * cfg.n_q_heads * cfg.head_dim
+    p = _ptr(q, "q", dt)
+    _here(q, "q")
+    if q.numel() == 0 or q.numel() % per:
+        raise ValueError(f"q has shape {tuple(q.shape)}: [batch, n, n_q_heads, head_dim] was expected")
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+    elif out.numel() != q.numel():
+        raise ValueError(f"out has {out.numel()} elements, expected {q.numel()}")
+    _here(out, "out")
+    _here(ws, "ws")
+    L.check(L.load().s4r_kv8_decode(_cfgp(cfg), c, n_tokens, _ints(lengths, "lengths", cfg.batch), q.numel() // per, p,
+                                    _ptr(out, "out", torch.float32), _ptr(ws, "ws", torch.uint8), ws.numel(),
+                                    _stream()))
     return out
 
 

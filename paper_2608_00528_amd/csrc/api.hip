@@ -16,6 +16,9 @@
 #include "s4r_internal.h"
 #include "select_key.h"
 
+static_assert(sizeof(s4r_kv8) == 40 && offsetof(s4r_kv8, k_codes) == 8 && S4R_KV8_BLOCK == s4r::kKv8Block,
+              "s4r_kv8 layout is part of the ABI");
+
 static_assert(sizeof(s4r_config) == 80 && offsetof(s4r_config, capacity) == 56 &&
                   offsetof(s4r_config, rank_v) == 72,
               "s4r_config layout is part of the ABI");
@@ -457,6 +460,168 @@ s4r_status s4r_dense_decode(const s4r_config* cfg, int64_t N, const void* q, con
   if ((st = check_ws(P, ws, ws_bytes))) return st;
   Workspace w = carve_workspace(P, ws);
   return hip_status(launch_dense_decode(P, w, N, q, k_cache, v_cache, out, stream), "s4r_dense_decode launch");
+}
+
+// ---- norms of the query and key heads, the 8-bit cache -----------------------------------
+namespace {
+
+bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
+
+#define S4R_INTS(ptr)                                                                    \
+  do {                                                                                   \
+    if (!aligned4(ptr)) return fail(S4R_ERR_MISALIGNED, "%s is not 4-byte aligned", #ptr); \
+  } while (0)
+
+// rows of `width` elements, `stride` elements apart
+s4r_status check_rows(const Problem& P, const char* name, int64_t stride, int64_t width) {
+  if (stride < width)
+    return fail(S4R_ERR_BAD_SHAPE, "%s stride %lld is smaller than a row of %lld", name, (long long)stride,
+                (long long)width);
+  if (stride > INT32_MAX) return fail(S4R_ERR_UNSUPPORTED, "%s stride %lld > %d", name, (long long)stride, INT32_MAX);
+  if (stride * elem_size(P) % 16)
+    return fail(S4R_ERR_MISALIGNED, "%s rows, %lld elements apart, are not 16-byte aligned", name, (long long)stride);
+  return S4R_OK;
+}
+
+s4r_status make_kv8(const Problem& P, const s4r_kv8* cache, Kv8& C) {
+  if (!cache) return fail(S4R_ERR_NULL_ARG, "cache is NULL");
+  if (cache->format != S4R_KV_INT8 && cache->format != S4R_KV_E4M3)
+    return fail(S4R_ERR_BAD_SHAPE, "cache format %d invalid", cache->format);
+  S4R_REQ(cache->k_codes);
+  S4R_REQ(cache->k_scales);
+  S4R_REQ(cache->v_codes);
+  S4R_REQ(cache->v_scales);
+  // grid dimensions of the cache's kernels
+  if (P.B > 32767 || P.hkv > 65535)
+    return fail(S4R_ERR_UNSUPPORTED, "batch %d > 32767 or %d KV heads > 65535", P.B, P.hkv);
+  if ((int64_t)P.B * P.hkv * kv8_tiles(P) > INT32_MAX / 2)
+    return fail(S4R_ERR_UNSUPPORTED, "a cache of %lld blocks per side is too large",
+                (long long)P.B * P.hkv * kv8_tiles(P));
+  C = Kv8{cache->format, (uint8_t*)cache->k_codes, cache->k_scales, (uint8_t*)cache->v_codes, cache->v_scales,
+          nullptr, nullptr, 0};
+  return S4R_OK;
+}
+
+// the token range of a write or read call
+s4r_status kv8_range(const Problem& P, Kv8& C, int64_t n_rows, int64_t row0, const int32_t* starts,
+                     const int32_t* counts) {
+  if (n_rows < 1 || n_rows > P.cap)
+    return fail(S4R_ERR_BAD_SHAPE, "n_rows = %lld outside [1, capacity = %lld]", (long long)n_rows, (long long)P.cap);
+  if (!starts && (row0 < 0 || row0 > P.cap || (!counts && row0 + n_rows > P.cap)))
+    return fail(S4R_ERR_BAD_SHAPE, "rows %lld .. %lld outside [0, capacity = %lld)", (long long)row0,
+                (long long)(row0 + n_rows - 1), (long long)P.cap);
+  S4R_INTS(starts);
+  S4R_INTS(counts);
+  C.starts = starts;
+  C.counts = counts;
+  C.row0 = starts ? 0 : row0;
+  return S4R_OK;
+}
+
+}  // namespace
+
+s4r_status s4r_qk_norm_rope(const s4r_config* cfg, int64_t n_tokens, const void* q, int64_t q_stride, const void* k,
+                            int64_t k_stride, const void* q_weight, const void* k_weight, float eps,
+                            const int32_t* positions, void* q_out, int64_t q_out_stride, void* k_out,
+                            int64_t k_out_stride, hipStream_t stream) {
+  Problem P;
+  s4r_status st = make_problem(cfg, P);
+  if (st) return st;
+  if (n_tokens < 1 || n_tokens > INT32_MAX)
+    return fail(S4R_ERR_BAD_SHAPE, "n_tokens = %lld outside [1, %d]", (long long)n_tokens, INT32_MAX);
+  if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(S4R_ERR_BAD_SHAPE, "eps must be finite and >= 0");
+  if (!q && !k) return fail(S4R_ERR_NULL_ARG, "q and k are both NULL");
+  if (!q != !q_out) return fail(S4R_ERR_NULL_ARG, "q and q_out: one of the two is NULL");
+  if (!k != !k_out) return fail(S4R_ERR_NULL_ARG, "k and k_out: one of the two is NULL");
+  if (q) {
+    S4R_REQ(q);
+    S4R_REQ(q_out);
+    if ((st = check_rows(P, "q", q_stride, (int64_t)P.hq * P.dh))) return st;
+    if ((st = check_rows(P, "q_out", q_out_stride, (int64_t)P.hq * P.dh))) return st;
+  }
+  if (k) {
+    S4R_REQ(k);
+    S4R_REQ(k_out);
+    if ((st = check_rows(P, "k", k_stride, (int64_t)P.Dp))) return st;
+    if ((st = check_rows(P, "k_out", k_out_stride, (int64_t)P.Dp))) return st;
+  }
+  S4R_OPT(q_weight);
+  S4R_OPT(k_weight);
+  if (P.theta != 0.f && !positions) return fail(S4R_ERR_NULL_ARG, "positions is NULL");
+  S4R_INTS(positions);
+  return hip_status(launch_qk_norm_rope(P, n_tokens, q, q_stride, k, k_stride, q_weight, k_weight, eps, positions,
+                                        q_out, q_out_stride, k_out, k_out_stride, stream),
+                    "s4r_qk_norm_rope launch");
+}
+
+s4r_status s4r_kv8_size(const s4r_config* cfg, size_t* code_bytes, size_t* scale_count) {
+  Problem P;
+  s4r_status st = make_problem(cfg, P);
+  if (st) return st;
+  if (!code_bytes || !scale_count) return fail(S4R_ERR_NULL_ARG, "code_bytes or scale_count is NULL");
+  *scale_count = (size_t)P.B * P.hkv * kv8_tiles(P);
+  *code_bytes = *scale_count * kKv8Block * P.dh;
+  return ok();
+}
+
+s4r_status s4r_kv8_write(const s4r_config* cfg, const s4r_kv8* cache, int64_t n_rows, int64_t row0,
+                         const int32_t* starts, const int32_t* counts, const void* k_rows, int64_t k_stride,
+                         const void* v_rows, int64_t v_stride, hipStream_t stream) {
+  Problem P;
+  Kv8 C;
+  s4r_status st = make_problem(cfg, P);
+  if (st) return st;
+  if ((st = make_kv8(P, cache, C)) || (st = kv8_range(P, C, n_rows, row0, starts, counts))) return st;
+  S4R_REQ(k_rows);
+  S4R_REQ(v_rows);
+  if ((st = check_rows(P, "k_rows", k_stride, P.Dp)) || (st = check_rows(P, "v_rows", v_stride, P.Dp))) return st;
+  return hip_status(launch_kv8_write(P, C, n_rows, k_rows, k_stride, v_rows, v_stride, stream),
+                    "s4r_kv8_write launch");
+}
+
+s4r_status s4r_kv8_read(const s4r_config* cfg, const s4r_kv8* cache, int64_t n_rows, int64_t row0,
+                        const int32_t* starts, const int32_t* counts, void* k_out, void* v_out, hipStream_t stream) {
+  Problem P;
+  Kv8 C;
+  s4r_status st = make_problem(cfg, P);
+  if (st) return st;
+  if ((st = make_kv8(P, cache, C)) || (st = kv8_range(P, C, n_rows, row0, starts, counts))) return st;
+  S4R_REQ(k_out);
+  S4R_REQ(v_out);
+  return hip_status(launch_kv8_read(P, C, n_rows, k_out, v_out, stream), "s4r_kv8_read launch");
+}
+
+static s4r_status check_queries(const Problem& P, int32_t n_q) {
+  if (n_q < 1) return fail(S4R_ERR_BAD_SHAPE, "n_q %d < 1", n_q);
+  if ((int64_t)n_q * P.G > kKv8MaxRows)
+    return fail(S4R_ERR_UNSUPPORTED, "n_q * G = %lld > %d not supported", (long long)n_q * P.G, kKv8MaxRows);
+  return S4R_OK;
+}
+
+s4r_status s4r_kv8_workspace_size(const s4r_config* cfg, int32_t n_q, size_t* bytes) {
+  Problem P;
+  s4r_status st = make_problem(cfg, P);
+  if (st) return st;
+  if ((st = check_queries(P, n_q))) return st;
+  if (!bytes) return fail(S4R_ERR_NULL_ARG, "bytes is NULL");
+  *bytes = align256(kv8_ws_bytes(P, n_q));
+  return ok();
+}
+
+s4r_status s4r_kv8_decode(const s4r_config* cfg, const s4r_kv8* cache, int64_t N, const int32_t* lengths, int32_t n_q,
+                          const void* q, float* out, void* ws, size_t ws_bytes, hipStream_t stream) {
+  Problem P;
+  Kv8 C;
+  s4r_status st = make_problem(cfg, P);
+  if (st) return st;
+  if ((st = make_kv8(P, cache, C)) || (st = check_queries(P, n_q))) return st;
+  if (N < 1 || N > P.cap)
+    return fail(S4R_ERR_BAD_SHAPE, "N = %lld outside [1, capacity = %lld]", (long long)N, (long long)P.cap);
+  S4R_INTS(lengths);
+  S4R_REQ(q);
+  S4R_REQ(out);
+  if ((st = check_ws(ws, ws_bytes, align256(kv8_ws_bytes(P, n_q))))) return st;
+  return hip_status(launch_kv8_decode(P, C, N, lengths, n_q, q, out, ws, stream), "s4r_kv8_decode launch");
 }
 
 s4r_status s4r_full_recon_decode(const s4r_config* cfg, int64_t L, const void* q, const void* sink_k,

@@ -1,0 +1,101 @@
+// The 8-bit KV cache: blocks of 64 tokens of one (sequence, KV head) with one
+// fp32 scale per block and side, in the order the attention kernel's MFMA
+// operands take them.
+//
+// A block is 64 * d_h contiguous bytes; 1 KiB pieces, one 16-byte load per lane.
+//   keys    (t / 16, d / 64, (d % 64) / 16, t % 16, d % 16): lane l of a piece
+//           holds token l % 16 and 16 dims of k-group l / 16;
+//   values  (d / 16, (t % 16) / 4, d % 16, t % 4, t / 16): lane l holds dim
+//           l % 16 and 16 tokens of k-group l / 16, the tokens 16 i + 4 (l / 16) + v
+//           at byte 4 v + i, which is how the logits' MFMA leaves the softmax
+//           weights in the lanes (row l % 16, tokens 4 (l / 16) + v of subtile i).
+#pragma once
+
+#include "s4r_device.h"
+#include "s4r_internal.h"
+
+namespace s4r {
+
+// the smallest block maximum that is stored; below it the block holds zeros (its
+// scale and the scale's reciprocal stay normal fp32 numbers)
+constexpr uint32_t kKv8MinBits = 0x12800000u;      // 2^-90
+
+__device__ __forceinline__ int key_offset(int t, int d, int dh) {
+  return (t >> 4) * (16 * dh) + (d >> 6) * 1024 + ((d & 63) >> 4) * 256 + (t & 15) * 16 + (d & 15);
+}
+__device__ __forceinline__ int value_offset(int t, int d) {
+  return (d >> 4) * 1024 + ((t & 15) >> 2) * 256 + (d & 15) * 16 + (t & 3) * 4 + (t >> 4);
+}
+
+// scale of a block whose largest |value| has these bits (NaN where a value is
+// not finite): int8 amax / 127 correctly rounded, e4m3 the smallest power of two
+// with amax <= 448 * scale (a power of two leaves x / scale exact)
+template <int FMT>
+__device__ __forceinline__ float kv8_scale(uint32_t amax_bits) {
+  if (amax_bits >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
+  if (amax_bits < kKv8MinBits) return 0.f;
+  if (FMT == S4R_KV_INT8) return __fdiv_rn(__uint_as_float(amax_bits), 127.f);
+  // 448 = 1.75 * 2^8: exponent of amax less 8, one more where the mantissa is above 1.75
+  const uint32_t e = (amax_bits >> 23) - 8u + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1u : 0u);
+  return __uint_as_float(e << 23);
+}
+// reciprocal used by kv8_code (0 where the block holds no values)
+template <int FMT>
+__device__ __forceinline__ float kv8_inverse(float s) {
+  if (!(s > 0.f)) return 0.f;
+  if (FMT == S4R_KV_INT8) return __fdiv_rn(1.f, s);
+  return __uint_as_float((254u << 23) - __float_as_uint(s));   // 2^-e
+}
+
+// nearest integer to x / s, ties to even, exactly: the product with the rounded
+// reciprocal is off by at most one step next to a tie, and the remainder
+// x - n s is exact in one fma (a multiple of ulp(s) / 2 no larger than s)
+__device__ __forceinline__ int kv8_nearest(float x, float s, float inv) {
+  float n = rintf(x * inv);
+  const float e = fmaf(-n, s, x), h = 0.5f * s;
+  if (fabsf(e) >= h) {
+    const float up = e > 0.f ? 1.f : -1.f;
+    // past the middle, or on it with n odd
+    if (fabsf(e) > h || ((int)n & 1)) n += up;
+  }
+  return (int)n;
+}
+// four codes, little endian
+template <int FMT>
+__device__ __forceinline__ uint32_t kv8_code4(float a, float b, float c, float d, float s, float inv) {
+  if (FMT == S4R_KV_INT8) {
+    if (inv == 0.f) return 0u;
+    const int ia = kv8_nearest(a, s, inv), ib = kv8_nearest(b, s, inv), ic = kv8_nearest(c, s, inv),
+              id = kv8_nearest(d, s, inv);
+    return (uint32_t)(ia & 255) | (uint32_t)(ib & 255) << 8 | (uint32_t)(ic & 255) << 16 | (uint32_t)id << 24;
+  }
+  if (inv == 0.f) return 0u;
+  int v = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, v, true);
+}
+// the four numbers that a dword of codes stands for, before the scale
+typedef float kv8_f2 __attribute__((ext_vector_type(2)));
+template <int FMT>
+__device__ __forceinline__ void kv8_numbers(uint32_t w, float (&x)[4]) {
+  if (FMT == S4R_KV_INT8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int)(int8_t)(w >> (8 * i));
+  } else {
+    const kv8_f2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    x[0] = lo[0];
+    x[1] = lo[1];
+    x[2] = hi[0];
+    x[3] = hi[1];
+  }
+}
+
+// rows a call writes to or reads from sequence b: [start, start + count), none
+// where they do not lie inside the cache
+__device__ __forceinline__ void kv8_rows(const int32_t* starts, const int32_t* counts, int b, int64_t row0, int n_rows,
+                                         int64_t cap, int64_t& start, int& count) {
+  start = starts ? (int64_t)starts[b] : row0;
+  count = counts ? min(max(counts[b], 0), n_rows) : n_rows;
+  if (start < 0 || start + count > cap) start = 0, count = 0;
+}
+
+}  // namespace s4r

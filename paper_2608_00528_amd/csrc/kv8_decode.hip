@@ -1,0 +1,493 @@
+// Attention of one or a few query tokens per sequence over the 8-bit KV cache
+// (layout: kv8.h).
+//
+//   s_t = (q . k_t) * scale_k(block) / sqrt(d_h),  p = exp(s - M),
+//   out = sum_t p_t scale_v(block) v_t / sum_t p_t
+//
+// with the running maximum M and sum of one pass over the tokens.  Bound by HBM:
+// 2 d_h bytes per token and KV head, so every other cost has to hide under the
+// stream:
+//  - the codes are operands as loaded (16 bytes per lane, 1 KiB per wave load) and
+//    become bf16 exactly; 16 query rows (query token x group member) share them;
+//  - logits as K q^T: 16 tokens x 16 query rows per MFMA, so lane l ends with
+//    query row l % 16 and the tokens 16 i + 4 (l / 16) + v of the block - which is
+//    the A operand of P V, with no exchange between lanes;
+//  - scales are one number per block: the logits' goes into the exponent's factor,
+//    the values' into p;
+//  - p keeps 24 bits as three bf16 parts (a truncated part of each remainder), so
+//    the products with the 8-bit codes are exact and sums are fp32.
+//
+// Work is split over a fixed number of workgroups by the tokens that are there: the
+// blocks of all (sequence, KV head) pairs in a row, an equal run of them for each
+// workgroup, whose four waves take the blocks in turn.  A pair inside one run is
+// finished there; one cut by the ends of runs leaves a partial (max, sum, output)
+// per run and k_kv8_combine merges them in order.  Lengths are read on the device,
+// so a captured graph follows them.
+#include "kv8.h"
+
+namespace s4r {
+namespace {
+
+constexpr int kWaves = 4;
+constexpr float kGrow = 6.f;            // the running maximum follows once a logit is 2^6 above it
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// eight codes -> eight bf16 values (exact)
+template <int FMT>
+__device__ __forceinline__ Op8 codes_to_bf16(uint32_t w0, uint32_t w1) {
+  Op8 o;
+  if (FMT == S4R_KV_INT8) {
+    float a[4], b[4];
+    kv8_numbers<FMT>(w0, a);
+    kv8_numbers<FMT>(w1, b);
+    o.u = make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3]));
+  } else {
+    o.u.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, false));
+    o.u.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, true));
+    o.u.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, false));
+    o.u.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, true));
+  }
+  return o;
+}
+
+// two fp32 values' upper halves as packed bf16 (truncated)
+__device__ __forceinline__ uint32_t upper2(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ float upper(float a) { return __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
+
+// max / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48
+__device__ __forceinline__ float rows_max(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float rows_sum(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// the sequences' tokens: lengths on the device (clamped to [0, n_max]) or n_max each
+struct Seqs {
+  const int32_t* lengths;
+  int n_max, B, hkv;
+  __device__ __forceinline__ int tokens(int b) const { return lengths ? min(max(lengths[b], 0), n_max) : n_max; }
+};
+__device__ __forceinline__ int blocks_of(int tokens) { return (tokens + kKv8Block - 1) / kKv8Block; }
+__device__ __forceinline__ int wave_scan(int x) {               // inclusive prefix sum over the lanes
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    const int y = __shfl_up(x, m);
+    if (lane >= m) x += y;
+  }
+  return x;
+}
+// blocks of all (sequence, KV head) pairs; every wave computes the same
+__device__ __forceinline__ int all_blocks(const Seqs& S) {
+  if (!S.lengths) return S.B * S.hkv * blocks_of(S.n_max);
+  int n = 0;
+  for (int b0 = 0; b0 < S.B; b0 += 64) {
+    const int b = b0 + (int)(threadIdx.x & 63);
+    n += __shfl(wave_scan(b < S.B ? blocks_of(S.tokens(b)) * S.hkv : 0), 63);
+  }
+  return n;
+}
+// blocks of one workgroup's run: a multiple of the waves
+__device__ __forceinline__ int run_of(int total, int nwg) { return ((total + nwg - 1) / nwg + kWaves - 1) / kWaves * kWaves; }
+// the sequence that holds block u of them all, and its first block
+__device__ __forceinline__ void find_sequence(const Seqs& S, int u, int& seq, int& begin) {
+  if (!S.lengths) {
+    const int per = S.hkv * blocks_of(S.n_max);
+    seq = u / per;
+    begin = seq * per;
+    return;
+  }
+  int n = 0;
+  seq = begin = 0;
+  for (int b0 = 0; b0 < S.B; b0 += 64) {
+    const int b = b0 + (int)(threadIdx.x & 63);
+    const int mine = b < S.B ? blocks_of(S.tokens(b)) * S.hkv : 0;
+    const int upto = n + wave_scan(mine);
+    const uint64_t past = __ballot(upto > u);
+    if (past) {
+      const int l = __ffsll((unsigned long long)past) - 1;
+      seq = b0 + l;
+      begin = __shfl(upto - mine, l);
+      return;
+    }
+    n = __shfl(upto, 63);
+  }
+}
+// blocks before sequence b
+__device__ __forceinline__ int blocks_before(const Seqs& S, int b) {
+  if (!S.lengths) return b * S.hkv * blocks_of(S.n_max);
+  int n = 0;
+  for (int b0 = 0; b0 < b; b0 += 64) {
+    const int i = b0 + (int)(threadIdx.x & 63);
+    n += __shfl(wave_scan(i < b ? blocks_of(S.tokens(i)) * S.hkv : 0), 63);
+  }
+  return n;
+}
+
+// query elements as bf16 parts: bf16 as stored, fp32 in three
+template <typename T>
+struct QParts;
+template <>
+struct QParts<uint16_t> {
+  static constexpr int n = 1;
+  __device__ __forceinline__ static void load(const uint16_t* p, Op8* o) { o[0].u = *reinterpret_cast<const uint4*>(p); }
+};
+template <>
+struct QParts<float> {
+  static constexpr int n = 3;
+  __device__ __forceinline__ static void load(const float* p, Op8* o) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    split_f32x8(x, o[0], o[1], o[2]);
+  }
+};
+
+// partials: run w leaves slot 2 w for a pair that began before the run and slot
+// 2 w + 1 for one that begins in it and goes on behind it; per slot, chunk of query
+// rows and row a (max, sum) and d_h sums
+__device__ __forceinline__ int64_t part_row(int slot, int chunks, int chunk, int row) {
+  return ((int64_t)slot * chunks + chunk) * kKv8Rows + row;
+}
+
+template <typename T, int FMT, int DH>
+__global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
+    const T* __restrict__ q, const uint8_t* __restrict__ k_codes, const float* __restrict__ k_scales,
+    const uint8_t* __restrict__ v_codes, const float* __restrict__ v_scales, float* __restrict__ part_ml,
+    float* __restrict__ part_o, float* __restrict__ out, Seqs S, int nwg, int chunks, int n_q, int G, int tiles) {
+  constexpr int NP = QParts<T>::n, NK = DH / 16, NV = DH / 16;   // 1 KiB pieces of a block per side
+  constexpr int KB = DH / 64;
+  // workgroups of one run's query chunks 8 ids apart: on one XCD, sharing its L2
+  const int id = blockIdx.x, chunk = (id >> 3) % chunks, w = (id >> 3) / chunks * 8 + (id & 7);
+  if (w >= nwg) return;
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int col = lane & 15, kg = lane >> 4;
+  const int hkv = S.hkv, hq = hkv * G, rows = n_q * G;
+  const int total = __builtin_amdgcn_readfirstlane(all_blocks(S)), run = run_of(total, nwg);
+  const int u0 = w * run, u1 = min(u0 + run, total);
+
+  __shared__ float wm[kWaves][kKv8Rows], wl[kWaves][kKv8Rows];
+  __shared__ float wo[kWaves][kKv8Rows][DH];
+
+  const int row = chunk * kKv8Rows + col;                       // this lane's query row in the logits
+  const int back = row < rows ? n_q - 1 - row / G : 0;          // tokens that its query token does not see yet
+  const float to_log2 = 1.4426950408889634f / sqrtf((float)DH);
+
+  for (int u = u0; u < u1;) {
+    int b, begin;
+    find_sequence(S, u, b, begin);
+    b = __builtin_amdgcn_readfirstlane(b);
+    begin = __builtin_amdgcn_readfirstlane(begin);
+    const int N = S.tokens(b), T_b = blocks_of(N);
+    const int j = (u - begin) / T_b, first = (u - begin) - j * T_b;
+    const int n = min(T_b - first, u1 - u);                     // blocks of this pair in this run
+    const int64_t at = ((int64_t)b * hkv + j) * tiles;
+    const u32x4* kp = reinterpret_cast<const u32x4*>(k_codes + at * (kKv8Block * DH)) + lane;
+    const u32x4* vp = reinterpret_cast<const u32x4*>(v_codes + at * (kKv8Block * DH)) + lane;
+    const float* ksp = k_scales + at;
+    const float* vsp = v_scales + at;
+
+    u32x4 kk[NK], vv[NV];
+    float sk, sv;
+    auto load_keys = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NK; ++i) kk[i] = __builtin_nontemporal_load(kp + (int64_t)tile * (kKv8Block * DH / 16) + i * 64);
+      sk = ksp[tile];
+    };
+    auto load_values = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) vv[i] = __builtin_nontemporal_load(vp + (int64_t)tile * (kKv8Block * DH / 16) + i * 64);
+      sv = vsp[tile];
+    };
+    float M = -INFINITY, l = 0.f;
+    floatx4 acc[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+    if (wave < n) {
+      int tile = first + wave;
+      const int last = first + wave + (n - 1 - wave) / kWaves * kWaves;
+      load_keys(tile);
+      load_values(tile);
+      Op8 qb[KB][2][NP];
+      {
+        const int r = min(row, rows - 1);
+        const T* qp = q + (((int64_t)b * n_q + r / G) * hq + (int64_t)j * G + r % G) * DH;
+#pragma unroll
+        for (int d = 0; d < KB; ++d)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) QParts<T>::load(qp + d * 64 + 16 * kg + 8 * h, qb[d][h]);
+      }
+      for (;; tile += kWaves) {
+        // logits
+        floatx4 s[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int d = 0; d < KB; ++d)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const Op8 a = codes_to_bf16<FMT>(kk[i * KB + d][2 * h], kk[i * KB + d][2 * h + 1]);
+#pragma unroll
+              for (int p = 0; p < NP; ++p) s[i] = mfma16x16x32(a, qb[d][h][p], s[i]);
+            }
+        }
+        const float f = sk * to_log2;
+        load_keys(min(tile + kWaves, last));                    // past the end: the last one again
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) s[i][v] *= f;
+        // tokens that a query row does not see (of the pair's last blocks only)
+        const int seen = N - back - tile * kKv8Block;           // this row sees the block's first `seen` tokens
+        const bool part = (tile + 1) * kKv8Block > N - (n_q - 1);
+        if (part) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) s[i][v] = (16 * i + 4 * kg + v < seen) ? s[i][v] : -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) top = fmaxf(top, s[i][v]);
+        top = rows_max(top);
+        const bool grow = top > M + kGrow;                      // also where M is -inf and a token is seen
+        if (__ballot(grow)) {
+          const float to = grow ? top : M;
+          const float a = grow ? __builtin_amdgcn_exp2f(M - to) : 1.f;
+          M = to;
+          l *= a;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float av = __shfl(a, 4 * kg + v);             // lane r holds row r
+#pragma unroll
+            for (int i = 0; i < NV; ++i) acc[i][v] *= av;
+          }
+        }
+        const float ref = M == -INFINITY ? 0.f : M;
+        float x[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const float p = __builtin_amdgcn_exp2f(s[i][v] - ref);
+            l += p;
+            x[i][v] = p * sv;
+          }
+        if (part) {
+          // a token that is not seen takes no part, whatever its block's scale or codes are
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) x[i][v] = (16 * i + 4 * kg + v < seen) ? x[i][v] : 0.f;
+          const int there = N - tile * kKv8Block;               // tokens of the block that exist
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m |= (16 * i + 4 * kg + v < there) ? 0xFFu << (8 * i) : 0u;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) vv[i][v] &= m;
+          }
+        }
+        // three parts of p * scale; contraction index 4 v + i of k-group kg
+        Op8 pa[2][3];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int p = 0; p < 3; ++p) {
+            uint32_t o[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int v = 2 * h + e / 2, i = 2 * (e % 2);
+              o[e] = upper2(x[i][v], x[i + 1][v]);
+              x[i][v] -= upper(x[i][v]);
+              x[i + 1][v] -= upper(x[i + 1][v]);
+            }
+            pa[h][p].u = make_uint4(o[0], o[1], o[2], o[3]);
+          }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const Op8 bv = codes_to_bf16<FMT>(vv[i][2 * h], vv[i][2 * h + 1]);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) acc[i] = mfma16x16x32(pa[h][p], bv, acc[i]);
+          }
+        if (tile == last) break;
+        load_values(tile + kWaves);
+      }
+    }
+    // merge the waves
+    const float ls = rows_sum(l);
+    if (kg == 0) {
+      wm[wave][col] = M;
+      wl[wave][col] = ls;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) wo[wave][4 * kg + v][16 * i + col] = acc[i][v];
+    __syncthreads();
+    const bool whole = first == 0 && n == T_b;
+    const int slot = first > 0 ? 2 * w : 2 * w + 1;
+    for (int e = t; e < kKv8Rows * DH; e += kWaves * 64) {
+      const int r = e / DH, d = e % DH, gr = chunk * kKv8Rows + r;
+      if (gr >= rows) break;
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) top = fmaxf(top, wm[i][r]);
+      float sum = 0.f, o = 0.f;
+#pragma unroll
+      for (int i = 0; i < kWaves; ++i) {
+        // a wave without a maximum has sums of zero, or NaN, which stay
+        const float a = wm[i][r] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(wm[i][r] - top);
+        sum += a * wl[i][r];
+        o += a * wo[i][r][d];
+      }
+      if (whole) {
+        out[(((int64_t)b * n_q + gr / G) * hq + (int64_t)j * G + gr % G) * DH + d] = sum == 0.f ? 0.f : o / sum;
+      } else {
+        const int64_t pr = part_row(slot, chunks, chunk, r);
+        part_o[pr * DH + d] = o;
+        if (d == 0) {
+          part_ml[pr * 2] = top;
+          part_ml[pr * 2 + 1] = sum;
+        }
+      }
+    }
+    __syncthreads();
+    u += n;
+  }
+}
+
+// merges the partials of the pairs that runs cut, and writes the zeros of sequences
+// without tokens.  One workgroup per query row of a sequence, groups of DH / 4
+// threads over the partials.
+template <int DH>
+__global__ __launch_bounds__(256) void k_kv8_combine(const float* __restrict__ part_ml, const float* __restrict__ part_o,
+                                                     float* __restrict__ out, Seqs S, int nwg, int chunks, int n_q,
+                                                     int G) {
+  constexpr int NG = 256 / (DH / 4);
+  const int gr = blockIdx.x, j = blockIdx.y, b = blockIdx.z;
+  const int t = threadIdx.x, g = t / (DH / 4), d4 = t % (DH / 4);
+  const int hq = S.hkv * G;
+  float4* dst = reinterpret_cast<float4*>(out + (((int64_t)b * n_q + gr / G) * hq + (int64_t)j * G + gr % G) * DH) + d4;
+  const int T_b = blocks_of(S.tokens(b));
+  if (T_b == 0) {
+    if (g == 0) *dst = make_float4(0.f, 0.f, 0.f, 0.f);
+    return;
+  }
+  const int run = run_of(all_blocks(S), nwg);
+  const int u0 = blocks_before(S, b) + j * T_b, u1 = u0 + T_b;
+  const int w0 = u0 / run, w1 = (u1 - 1) / run;
+  if (w0 == w1) return;                                         // finished by its run
+  const int chunk = gr / kKv8Rows, row = gr % kKv8Rows;
+  auto slot = [&](int w) { return part_row(w == w0 ? 2 * w + 1 : 2 * w, chunks, chunk, row); };
+  float M = -INFINITY;
+  for (int w = w0 + t; w <= w1; w += 256) M = fmaxf(M, part_ml[slot(w) * 2]);
+  __shared__ float sm[4];
+  __shared__ float4 so[NG][DH / 4];
+  __shared__ float sl[NG];
+  M = wave_max(M);
+  if ((t & 63) == 0) sm[t >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int w = w0 + g; w <= w1; w += NG) {
+    const int64_t pr = slot(w);
+    const float m = part_ml[pr * 2], pl = part_ml[pr * 2 + 1];
+    const float4 x = reinterpret_cast<const float4*>(part_o + pr * DH)[d4];
+    const float a = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);
+    l += a * pl;
+    o.x += a * x.x, o.y += a * x.y, o.z += a * x.z, o.w += a * x.w;
+  }
+  so[g][d4] = o;
+  if (d4 == 0) sl[g] = l;
+  __syncthreads();
+  if (g == 0) {
+    l = 0.f;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      l += sl[i];
+      const float4 x = so[i][d4];
+      o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
+    }
+    const float r = l == 0.f ? 0.f : 1.f / l;
+    *dst = make_float4(o.x * r, o.y * r, o.z * r, o.w * r);
+  }
+}
+
+int row_chunks(const Problem& P, int n_q) { return (n_q * P.G + kKv8Rows - 1) / kKv8Rows; }
+// runs of a call over at most n_max tokens per sequence: a block for every wave at least
+int runs(const Problem& P, int n_q, int64_t n_max) {
+  const int64_t blocks = (int64_t)P.B * P.hkv * ((n_max + kKv8Block - 1) / kKv8Block);
+  return (int)std::max<int64_t>(1, std::min<int64_t>((blocks + kWaves - 1) / kWaves, kKv8Wgs / row_chunks(P, n_q)));
+}
+
+}  // namespace
+
+// (max, sum) and d_h sums for two slots per run, sixteen rows per chunk
+size_t kv8_ws_bytes(const Problem& P, int n_q) {
+  const size_t part_rows = (size_t)2 * runs(P, n_q, P.cap) * row_chunks(P, n_q) * kKv8Rows;
+  return part_rows * (P.dh + 2) * sizeof(float);
+}
+
+hipError_t launch_kv8_decode(const Problem& P, const Kv8& C, int64_t n_max, const int32_t* lengths, int n_q,
+                             const void* q, float* out, void* ws, hipStream_t st) {
+  const int nwg = runs(P, n_q, n_max), chunks = row_chunks(P, n_q);
+  const size_t part_rows = (size_t)2 * nwg * chunks * kKv8Rows;
+  float* part_o = (float*)ws;
+  float* part_ml = part_o + part_rows * P.dh;
+  const Seqs S{lengths, (int)n_max, P.B, P.hkv};
+  const dim3 grid((nwg + 7) / 8 * 8 * chunks);
+  auto go = [&](auto elem, auto fmt, auto dh) {
+    using T = decltype(elem);
+    hipLaunchKernelGGL((k_kv8_decode<T, fmt(), dh()>), grid, dim3(kWaves * 64), 0, st, (const T*)q, C.k_codes, C.k_scales,
+                       C.v_codes, C.v_scales, part_ml, part_o, out, S, nwg, chunks, n_q, P.G, kv8_tiles(P));
+  };
+  auto by_fmt = [&](auto elem, auto dh) {
+    if (C.format == S4R_KV_INT8)
+      go(elem, std::integral_constant<int, S4R_KV_INT8>(), dh);
+    else
+      go(elem, std::integral_constant<int, S4R_KV_E4M3>(), dh);
+  };
+  auto by_type = [&](auto dh) {
+    if (P.dtype == S4R_BF16)
+      by_fmt(uint16_t(), dh);
+    else
+      by_fmt(float(), dh);
+  };
+  if (P.dh == 128)
+    by_type(std::integral_constant<int, 128>());
+  else
+    by_type(std::integral_constant<int, 64>());
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  // no pair is cut where every run holds whole pairs of equal length
+  const int64_t per = (n_max + kKv8Block - 1) / kKv8Block, total = per * P.B * P.hkv;
+  const int64_t run = ((total + nwg - 1) / nwg + kWaves - 1) / kWaves * kWaves;
+  if (!lengths && run % per == 0) return hipSuccess;
+  const dim3 cgrid(n_q * P.G, P.hkv, P.B);
+  if (P.dh == 128)
+    hipLaunchKernelGGL(k_kv8_combine<128>, cgrid, dim3(256), 0, st, part_ml, part_o, out, S, nwg, chunks, n_q, P.G);
+  else
+    hipLaunchKernelGGL(k_kv8_combine<64>, cgrid, dim3(256), 0, st, part_ml, part_o, out, S, nwg, chunks, n_q, P.G);
+  return hipGetLastError();
+}
+
+}  // namespace s4r

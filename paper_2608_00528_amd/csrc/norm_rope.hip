@@ -1,0 +1,170 @@
+// Norms of the query and key heads with the position rotation, in one pass:
+//
+//   y = x / sqrt(mean(x^2) + eps) * w   (per head; without a weight y = x)
+//   (y_i, y_{i + d_h/2}) turned by pos * theta^(-2 i / d_h)
+//
+// Reads and writes each element once: bound by HBM for a prompt, by one launch's
+// latency for a few tokens.  A lane holds dims 4 p .. + 3 and their partners
+// d_h / 2 above them, so the rotation stays in the lane and d_h / 8 lanes hold a
+// head; a wave takes 512 / d_h heads at a time and keeps the turns of its token over
+// all its heads.  Sums of squares are fp64 (no fp32 value's square overflows).
+#include "s4r_device.h"
+#include "s4r_internal.h"
+
+namespace s4r {
+namespace {
+
+__device__ __forceinline__ void load4(const uint16_t* p, float* x) {
+  const uint2 u = *reinterpret_cast<const uint2*>(p);
+  x[0] = __uint_as_float(u.x << 16);
+  x[1] = __uint_as_float(u.x & 0xFFFF0000u);
+  x[2] = __uint_as_float(u.y << 16);
+  x[3] = __uint_as_float(u.y & 0xFFFF0000u);
+}
+__device__ __forceinline__ void load4(const float* p, float* x) {
+  const float4 u = *reinterpret_cast<const float4*>(p);
+  x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w;
+}
+__device__ __forceinline__ void store4(uint16_t* p, const float* x) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+}
+__device__ __forceinline__ void store4(float* p, const float* x) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+}
+
+// sum over the d_h / 8 lanes of a head (every one of them gets it)
+template <int DH>
+__device__ __forceinline__ double head_sum(double x) {
+  x += dpp_d<0xB1>(x);                  // quad_perm [1,0,3,2]
+  x += dpp_d<0x4E>(x);                  // quad_perm [2,3,0,1]
+  x += dpp_d<0x141>(x);                 // row_half_mirror: the other quad of eight lanes
+  if (DH == 128) x += dpp_d<0x128>(x);  // row_ror:8
+  return x;
+}
+
+// cos and sin of pos * F revolutions; F a 0.64 fixed-point number, so the fraction
+// of a revolution is exact in 64-bit integer arithmetic for any position
+__device__ __forceinline__ void turn(int32_t pos, uint64_t F, float& c, float& s) {
+  const uint64_t phase = (uint64_t)(int64_t)pos * F;
+  const float x = (float)(int32_t)(phase >> 32) * 2.3283064365386963e-10f;   // revolutions in [-1/2, 1/2)
+  c = __builtin_amdgcn_cosf(x);
+  s = __builtin_amdgcn_sinf(x);
+}
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void k_qk_norm_rope(const T* q, int64_t q_stride, const T* k, int64_t k_stride,
+                                                      const T* __restrict__ q_weight,
+                                                      const T* __restrict__ k_weight, double eps,
+                                                      const int32_t* __restrict__ positions, T* q_out,
+                                                      int64_t q_out_stride, T* k_out, int64_t k_out_stride,
+                                                      int64_t n_tokens, int hq, int heads, int per, double ratio) {
+  constexpr int LPH = DH / 8, HPW = 64 / LPH;         // lanes per head, heads a wave takes at a time
+  const int lane = threadIdx.x & 63, p = lane % LPH, hl = lane / LPH;
+  const int d0 = 4 * p, d1 = d0 + DH / 2;
+  // this lane's frequencies as revolutions per position
+  uint64_t F[4] = {0, 0, 0, 0};
+  if (ratio != 0.0) {
+    double f = 1.0, base = ratio;
+    for (int e = d0; e > 0; e >>= 1) {
+      if (e & 1) f *= base;
+      base *= base;
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const double rev = f * 0.15915494309189535;
+      F[v] = (uint64_t)((rev - floor(rev)) * 18446744073709551616.0);
+      f *= ratio;
+    }
+  }
+  float wq[8], wk[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) wq[e] = wk[e] = 1.f;
+  if (q_weight) load4(q_weight + d0, wq), load4(q_weight + d1, wq + 4);
+  if (k_weight) load4(k_weight + d0, wk), load4(k_weight + d1, wk + 4);
+
+  // a unit: `per` groups of HPW heads of one token
+  const int groups = (heads + HPW - 1) / HPW, parts = (groups + per - 1) / per;
+  const int64_t units = n_tokens * parts;
+  const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), waves = (int64_t)gridDim.x * 4;
+  for (int64_t u = wave; u < units; u += waves) {
+    const int64_t tok = u / parts;
+    const int g0 = (int)(u - tok * parts) * per, g1 = min(g0 + per, groups);
+    float c[4], s[4];
+    if (ratio != 0.0) {
+      const int32_t pos = positions[tok];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) turn(pos, F[v], c[v], s[v]);
+    }
+    for (int g = g0; g < g1; ++g) {
+      const int h = g * HPW + hl;
+      if (h >= heads) continue;                       // whole groups of LPH lanes
+      const bool is_q = h < hq;
+      const T* src = is_q ? q + tok * q_stride + (int64_t)h * DH : k + tok * k_stride + (int64_t)(h - hq) * DH;
+      T* dst = is_q ? q_out + tok * q_out_stride + (int64_t)h * DH : k_out + tok * k_out_stride + (int64_t)(h - hq) * DH;
+      float x[8];
+      load4(src + d0, x);
+      load4(src + d1, x + 4);
+      if (is_q ? q_weight != nullptr : k_weight != nullptr) {
+        double ss = 0.0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) ss = fma((double)x[e], (double)x[e], ss);
+        const double ms = head_sum<DH>(ss) * (1.0 / DH) + eps;
+        // 1 / sqrt(ms): the hardware's estimate and two Newton steps
+        double r = __builtin_amdgcn_rsq(ms);
+        if (ms > 0.0 && ms < INFINITY) {
+          r *= 1.5 - 0.5 * ms * r * r;
+          r *= 1.5 - 0.5 * ms * r * r;
+        }
+        // values above 2^100 and their reciprocals stay normal fp32 numbers
+        const bool large = ms > 0x1p200;
+        const float pre = large ? 0x1p-100f : 1.f, rf = (float)(large ? r * 0x1p100 : r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x[e] * pre * rf * (is_q ? wq[e] : wk[e]);
+      }
+      if (ratio != 0.0) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float a = x[v], b = x[4 + v];
+          x[v] = a * c[v] - b * s[v];
+          x[4 + v] = b * c[v] + a * s[v];
+        }
+      }
+      store4(dst + d0, x);
+      store4(dst + d1, x + 4);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_qk_norm_rope(const Problem& P, int64_t n_tokens, const void* q, int64_t q_stride, const void* k,
+                               int64_t k_stride, const void* q_weight, const void* k_weight, float eps,
+                               const int32_t* positions, void* q_out, int64_t q_out_stride, void* k_out,
+                               int64_t k_out_stride, hipStream_t st) {
+  const int hq = q ? P.hq : 0, heads = hq + (k ? P.hkv : 0);
+  const int hpw = 512 / P.dh, groups = (heads + hpw - 1) / hpw;
+  // few tokens: a wave for each group of heads; many: a token's heads in one wave,
+  // which then works out the token's turns once
+  const int per = n_tokens * groups <= 4096 ? 1 : groups;
+  const int64_t units = n_tokens * ((groups + per - 1) / per);
+  const dim3 grid((unsigned)std::min<int64_t>((units + 3) / 4, 2048));
+  auto go = [&](auto elem, auto dh) {
+    using T = decltype(elem);
+    hipLaunchKernelGGL((k_qk_norm_rope<T, dh()>), grid, dim3(256), 0, st, (const T*)q, q_stride, (const T*)k, k_stride,
+                       (const T*)q_weight, (const T*)k_weight, (double)eps, positions, (T*)q_out, q_out_stride,
+                       (T*)k_out, k_out_stride, n_tokens, hq, heads, per, rope_ratio(P));
+  };
+  auto by_type = [&](auto dh) {
+    if (P.dtype == S4R_BF16)
+      go(uint16_t(), dh);
+    else
+      go(float(), dh);
+  };
+  if (P.dh == 128)
+    by_type(std::integral_constant<int, 128>());
+  else
+    by_type(std::integral_constant<int, 64>());
+  return hipGetLastError();
+}
+
+}  // namespace s4r

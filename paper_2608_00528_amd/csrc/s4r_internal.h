@@ -114,6 +114,23 @@ inline int qimg_mfmas(const Problem& P) { return std::min((P.GW + 3) / 4, kColBl
 // RoPE: ratio of consecutive frequencies theta^(-2 / d_h) (0 when RoPE is off)
 inline double rope_ratio(const Problem& P) { return P.theta == 0.f ? 0.0 : pow((double)P.theta, -2.0 / P.dh); }
 
+// ---- the 8-bit KV cache ----------------------------------------------------
+constexpr int kKv8Block = 64;         // tokens per block (one scale per side and KV head)
+constexpr int kKv8Rows = 16;          // query rows (query token x group member) per attention workgroup
+constexpr int kKv8MaxRows = 128;      // n_q * G
+constexpr int kKv8Wgs = 512;          // attention workgroups: two per CU
+struct Kv8 {
+  int format;                         // S4R_KV_INT8 | S4R_KV_E4M3
+  uint8_t* k_codes;                   // [B][hkv][tiles][64 * dh]
+  float* k_scales;                    // [B][hkv][tiles]
+  uint8_t* v_codes;
+  float* v_scales;
+  const int32_t* starts;              // device [B] or null: row0 for every sequence
+  const int32_t* counts;              // device [B] or null: every row of the call
+  int64_t row0;
+};
+inline int kv8_tiles(const Problem& P) { return (int)((P.cap + kKv8Block - 1) / kKv8Block); }
+
 // ---- launchers (each returns hipGetLastError() after its launches) --------
 
 // coefficient projections of Section 3.2.1: the query groups (fp32 c_t^Q
@@ -188,6 +205,18 @@ hipError_t launch_sparse_attn(const Problem& P, const Workspace& ws, int64_t L, 
                               const int32_t* idx, const float* k_sel, const float* v_sel,
                               float* out, hipStream_t st);
 bool attention_supported(const Problem& P);
+// norms of the query and key heads with the rotation (norm_rope.hip)
+hipError_t launch_qk_norm_rope(const Problem& P, int64_t n_tokens, const void* q, int64_t q_stride, const void* k,
+                               int64_t k_stride, const void* q_weight, const void* k_weight, float eps,
+                               const int32_t* positions, void* q_out, int64_t q_out_stride, void* k_out,
+                               int64_t k_out_stride, hipStream_t st);
+// the 8-bit cache: rows in and out (kv8.hip), attention over it (kv8_decode.hip)
+hipError_t launch_kv8_write(const Problem& P, const Kv8& C, int64_t n_rows, const void* k_rows, int64_t k_stride,
+                            const void* v_rows, int64_t v_stride, hipStream_t st);
+hipError_t launch_kv8_read(const Problem& P, const Kv8& C, int64_t n_rows, void* k_out, void* v_out, hipStream_t st);
+size_t kv8_ws_bytes(const Problem& P, int n_q);
+hipError_t launch_kv8_decode(const Problem& P, const Kv8& C, int64_t n_max, const int32_t* lengths, int n_q,
+                             const void* q, float* out, void* ws, hipStream_t st);
 // read-bandwidth reference: XOR of every word, one value per thread in sink
 int read_bandwidth_threads();
 hipError_t launch_read_all(const void* buf, int64_t n16, uint32_t* sink, hipStream_t st);
