@@ -492,8 +492,10 @@ s4r_status make_kv8(const Problem& P, const s4r_kv8* cache, Kv8& C) {
   S4R_REQ(cache->v_codes);
   S4R_REQ(cache->v_scales);
   // grid dimensions of the cache's kernels
-  if (P.B > 32767 || P.hkv > 65535)
-    return fail(S4R_ERR_UNSUPPORTED, "batch %d > 32767 or %d KV heads > 65535", P.B, P.hkv);
+  if (P.B > 32767) return fail(S4R_ERR_UNSUPPORTED, "batch %d > 32767", P.B);
+  if ((int64_t)P.hkv * (kv8_tiles(P) + 1) > UINT32_MAX / (2 * 128))
+    return fail(S4R_ERR_UNSUPPORTED, "%lld blocks per sequence and side are too many",
+                (long long)P.hkv * kv8_tiles(P));
   if ((int64_t)P.B * P.hkv * kv8_tiles(P) > INT32_MAX / 2)
     return fail(S4R_ERR_UNSUPPORTED, "a cache of %lld blocks per side is too large",
                 (long long)P.B * P.hkv * kv8_tiles(P));

@@ -39,7 +39,7 @@ __device__ __forceinline__ float kv8_scale(uint32_t amax_bits) {
   const uint32_t e = (amax_bits >> 23) - 8u + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1u : 0u);
   return __uint_as_float(e << 23);
 }
-// reciprocal used by kv8_code (0 where the block holds no values)
+// reciprocal used by the codes (0 where the block holds no values)
 template <int FMT>
 __device__ __forceinline__ float kv8_inverse(float s) {
   if (!(s > 0.f)) return 0.f;
@@ -47,31 +47,55 @@ __device__ __forceinline__ float kv8_inverse(float s) {
   return __uint_as_float((254u << 23) - __float_as_uint(s));   // 2^-e
 }
 
-// nearest integer to x / s, ties to even, exactly: the product with the rounded
-// reciprocal is off by at most one step next to a tie, and the remainder
-// x - n s is exact in one fma (a multiple of ulp(s) / 2 no larger than s)
-__device__ __forceinline__ int kv8_nearest(float x, float s, float inv) {
-  float n = rintf(x * inv);
-  const float e = fmaf(-n, s, x), h = 0.5f * s;
-  if (fabsf(e) >= h) {
-    const float up = e > 0.f ? 1.f : -1.f;
-    // past the middle, or on it with n odd
-    if (fabsf(e) > h || ((int)n & 1)) n += up;
-  }
-  return (int)n;
+// int8 codes of four numbers, little endian: the nearest integers to x / s, ties to
+// even, exactly.  fma(x, 1 / s, 1.5 * 2^23) rounds to an integer n in one step (its low
+// byte is the code) and is off by at most one, next to a tie only; the remainder
+// x - n s is exact in one fma (a multiple of ulp(s) / 2 no larger than s), so `worst`,
+// the largest |remainder|, says whether any of the numbers has to be looked at again:
+// about one in 10^5 does.
+constexpr float kKv8Round = 12582912.f;
+typedef uint32_t kv8_u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t kv8_u2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t kv8_low_bytes(float a, float b, float c, float d) {
+  const uint32_t ab = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x0C0C0400u);
+  const uint32_t cd = __builtin_amdgcn_perm(__float_as_uint(d), __float_as_uint(c), 0x04000C0Cu);
+  return ab | cd;
 }
-// four codes, little endian
-template <int FMT>
-__device__ __forceinline__ uint32_t kv8_code4(float a, float b, float c, float d, float s, float inv) {
-  if (FMT == S4R_KV_INT8) {
-    if (inv == 0.f) return 0u;
-    const int ia = kv8_nearest(a, s, inv), ib = kv8_nearest(b, s, inv), ic = kv8_nearest(c, s, inv),
-              id = kv8_nearest(d, s, inv);
-    return (uint32_t)(ia & 255) | (uint32_t)(ib & 255) << 8 | (uint32_t)(ic & 255) << 16 | (uint32_t)id << 24;
+__device__ __forceinline__ uint32_t kv8_int8x4(float a, float b, float c, float d, float s, float inv, float& worst) {
+  const float x[4] = {a, b, c, d};
+  float n[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    n[i] = fmaf(x[i], inv, kKv8Round);
+    worst = fmaxf(worst, fabsf(fmaf(kKv8Round - n[i], s, x[i])));
   }
-  if (inv == 0.f) return 0u;
-  int v = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+  return kv8_low_bytes(n[0], n[1], n[2], n[3]);
+}
+// the same with every remainder looked at: past the middle, or on it with n odd,
+// the neighbour is the nearest (or the even one)
+__device__ __forceinline__ uint32_t kv8_int8x4_exact(float a, float b, float c, float d, float s, float inv) {
+  const float x[4] = {a, b, c, d};
+  float n[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    n[i] = fmaf(x[i], inv, kKv8Round);
+    const float e = fmaf(kKv8Round - n[i], s, x[i]), h = 0.5f * s;
+    if (fabsf(e) > h || (fabsf(e) == h && (__float_as_uint(n[i]) & 1u))) n[i] += e > 0.f ? 1.f : -1.f;
+  }
+  return kv8_low_bytes(n[0], n[1], n[2], n[3]);
+}
+__device__ __forceinline__ uint32_t kv8_e4m3x4(float a, float b, float c, float d, float inv) {
+  const int v = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, v, true);
+}
+// 4 x 4 bytes turned: byte i of r[j] from byte j of w[i]
+__device__ __forceinline__ void kv8_turn4(const uint32_t* w, uint32_t* r) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u),
+                 c = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  r[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+  r[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+  r[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+  r[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 // the four numbers that a dword of codes stands for, before the scale
 typedef float kv8_f2 __attribute__((ext_vector_type(2)));

@@ -14,55 +14,86 @@ namespace {
 
 // eight consecutive elements of a row
 __device__ __forceinline__ void load8(const uint16_t* p, float (&x)[8]) {
-  const uint4 u = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  const kv8_u4 u = *reinterpret_cast<const kv8_u4*>(p);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    x[2 * i] = __uint_as_float(u[i] << 16);
+    x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
   }
 }
 __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  const floatx4 a = *reinterpret_cast<const floatx4*>(p), b = *reinterpret_cast<const floatx4*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
 }
 __device__ __forceinline__ void store8(uint16_t* p, const float (&x)[8]) {
-  *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                                            pack_bf16x2(x[6], x[7]));
+  const kv8_u4 u = {pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+  __builtin_nontemporal_store(u, reinterpret_cast<kv8_u4*>(p));
 }
 __device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
-  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+  __builtin_nontemporal_store(floatx4{x[0], x[1], x[2], x[3]}, reinterpret_cast<floatx4*>(p));
+  __builtin_nontemporal_store(floatx4{x[4], x[5], x[6], x[7]}, reinterpret_cast<floatx4*>(p + 4));
 }
 
-// the numbers of this thread's pieces of a block image, x[i][e]: token 16 i + c, dim 8 dc + e
-template <int FMT, int DH>
-__device__ __forceinline__ void pieces_of(const uint8_t* img, bool keys, int c, int dc, float (&x)[4][8]) {
+// this thread's codes in a block image: w[e] holds dim 8 dc + e of the tokens c, 16 + c,
+// 32 + c, 48 + c (a dword of the value order; turned from and to the key order's
+// 8 bytes per token)
+template <int DH>
+__device__ __forceinline__ void get_codes(const uint8_t* img, bool keys, int c, int dc, uint32_t (&w)[8]) {
   if (keys) {
+    uint32_t lo[4], hi[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const uint2 w = *reinterpret_cast<const uint2*>(img + key_offset(16 * i + c, 8 * dc, DH));
-      float a[4], b[4];
-      kv8_numbers<FMT>(w.x, a);
-      kv8_numbers<FMT>(w.y, b);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[i][e] = a[e], x[i][4 + e] = b[e];
+      const kv8_u2 u = *reinterpret_cast<const kv8_u2*>(img + key_offset(16 * i + c, 8 * dc, DH));
+      lo[i] = u[0];
+      hi[i] = u[1];
     }
+    kv8_turn4(lo, w);
+    kv8_turn4(hi, w + 4);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float a[4];
-      kv8_numbers<FMT>(*reinterpret_cast<const uint32_t*>(img + value_offset(c, 8 * dc + e)), a);
+    for (int e = 0; e < 8; ++e) w[e] = *reinterpret_cast<const uint32_t*>(img + value_offset(c, 8 * dc + e));
+  }
+}
+template <int DH>
+__device__ __forceinline__ void put_codes(uint8_t* img, bool keys, int c, int dc, const uint32_t (&w)[8]) {
+  if (keys) {
+    uint32_t lo[4], hi[4];
+    kv8_turn4(w, lo);
+    kv8_turn4(w + 4, hi);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i][e] = a[i];
-    }
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<kv8_u2*>(img + key_offset(16 * i + c, 8 * dc, DH)) = kv8_u2{lo[i], hi[i]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) *reinterpret_cast<uint32_t*>(img + value_offset(c, 8 * dc + e)) = w[e];
   }
 }
 
 __device__ __forceinline__ uint32_t wave_max_u32(uint32_t x) {
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) x = max(x, (uint32_t)__shfl_xor((int)x, m));
-  return x;
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xF, 0xF, false));    // quad_perm [1,0,3,2]
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xF, 0xF, false));    // quad_perm [2,3,0,1]
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x124, 0xF, 0xF, false));   // row_ror:4
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xF, 0xF, false));   // row_ror:8
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = max((uint32_t)a[0], (uint32_t)a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return max((uint32_t)b[0], (uint32_t)b[1]);
+}
+
+// workgroup -> (head, block of the call, sequence, side); the heads of a block next to
+// each other, so the rows are read and written whole
+struct Place {
+  int j, blk, b;
+  bool keys;
+};
+__device__ __forceinline__ Place place(int hkv) {
+  Place p;
+  p.blk = blockIdx.x / hkv;
+  p.j = blockIdx.x - p.blk * hkv;
+  p.keys = blockIdx.y == 0;
+  p.b = blockIdx.z;
+  return p;
 }
 
 template <typename T, int FMT, int DH>
@@ -72,53 +103,49 @@ __global__ __launch_bounds__(DH * 2) void k_kv8_write(const T* __restrict__ k_ro
                                                       uint8_t* __restrict__ v_codes, float* __restrict__ v_scales,
                                                       const int32_t* __restrict__ starts,
                                                       const int32_t* __restrict__ counts, int64_t row0, int n_rows,
-                                                      int64_t cap, int tiles) {
+                                                      int64_t cap, int tiles, int hkv) {
   constexpr int NT = DH * 2, NW = NT / 64;
-  const int j = blockIdx.y, b = blockIdx.z >> 1, hkv = gridDim.y;
-  const bool keys = (blockIdx.z & 1) == 0;
+  const Place at = place(hkv);
+  const bool keys = at.keys;
   const int t = threadIdx.x, c = t / (DH / 8), dc = t % (DH / 8);
   int64_t start;
   int count;
-  kv8_rows(starts, counts, b, row0, n_rows, cap, start, count);
-  const int64_t tile = start / kKv8Block + blockIdx.x;
+  kv8_rows(starts, counts, at.b, row0, n_rows, cap, start, count);
+  const int64_t tile = start / kKv8Block + at.blk;
   const int64_t first = tile * kKv8Block - start;              // the block's first token among the call's rows
   if (first >= count) return;
   const int lo = first < 0 ? (int)-first : 0;                  // tokens [lo, hi) of the block are written
   const int hi = (int)min<int64_t>(kKv8Block, count - first);
-  const int64_t at = ((int64_t)b * hkv + j) * tiles + tile;
-  uint8_t* codes = (keys ? k_codes : v_codes) + at * (kKv8Block * DH);
-  float* scale = (keys ? k_scales : v_scales) + at;
-  const T* rows = keys ? k_rows : v_rows;
+  const int64_t blk = ((int64_t)at.b * hkv + at.j) * tiles + tile;
+  kv8_u4* codes = reinterpret_cast<kv8_u4*>((keys ? k_codes : v_codes) + blk * (kKv8Block * DH)) + t;
+  float* scale = (keys ? k_scales : v_scales) + blk;
   const int64_t stride = keys ? k_stride : v_stride;
+  const T* rows = (keys ? k_rows : v_rows) + ((int64_t)at.b * n_rows + first) * stride + (int64_t)at.j * DH + 8 * dc;
 
   __shared__ __align__(16) uint8_t img[kKv8Block * DH];
   __shared__ uint32_t wave_top[NW];
+  kv8_u4* image = reinterpret_cast<kv8_u4*>(img) + t;
   const bool whole = lo == 0 && hi == kKv8Block;
-  uint4 old[2];
+  kv8_u4 old0 = {0, 0, 0, 0}, old1 = old0;
   float s_old = 0.f;
   if (!whole) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) old[i] = reinterpret_cast<const uint4*>(codes)[t + i * NT];
-    if (lo > 0) s_old = *scale;
+    old0 = codes[0];
+    old1 = codes[NT];
+    s_old = *scale;
   }
   float x[4][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) load8(rows + min(max(16 * i + c, lo), hi - 1) * stride, x[i]);   // a row that is there
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = min(max(16 * i + c, lo), hi - 1);            // a row that is there, masked below
-    load8(rows + ((int64_t)b * n_rows + first + r) * stride + (int64_t)j * DH + 8 * dc, x[i]);
-  }
-#pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (16 * i + c >= lo && 16 * i + c < hi) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[i][e]) & 0x7FFFFFFFu);
-    }
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[i][e]) & 0x7FFFFFFFu);        // repeats change nothing
   top = wave_max_u32(top);
   if ((t & 63) == 0) wave_top[t >> 6] = top;
   if (!whole) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) reinterpret_cast<uint4*>(img)[t + i * NT] = old[i];
+    image[0] = old0;
+    image[NT] = old1;
   }
   __syncthreads();
 #pragma unroll
@@ -126,44 +153,53 @@ __global__ __launch_bounds__(DH * 2) void k_kv8_write(const T* __restrict__ k_ro
   float s = kv8_scale<FMT>(top);
   if (lo > 0) s = (s != s || s_old != s_old) ? __uint_as_float(0x7FC00000u) : fmaxf(s, s_old);
   const float inv = kv8_inverse<FMT>(s);
-  // the tokens of this thread that stay as they are: those past the last written,
-  // and the older ones unless the scale grew
-  uint32_t keep = 0;
+  // bytes of this thread's codes that stay as they are: the tokens past the last
+  // written, and the older ones unless the scale grew
+  uint32_t keep = 0, w_old[8];
   if (!whole) {
-    const bool redo = lo > 0 && !(s == s_old);
-    float z[4][8];
-    pieces_of<FMT, DH>(img, keys, c, dc, z);
+    get_codes<DH>(img, keys, c, dc, w_old);
+    const bool redo = !(s == s_old);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int r = 16 * i + c;
       if (r >= hi || (r < lo && !redo)) keep |= 0xFFu << (8 * i);
-      if (r < lo) {
+    }
+    if (lo > 0 && redo) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = z[i][e] * s_old;
+      for (int e = 0; e < 8; ++e) {
+        float z[4];
+        kv8_numbers<FMT>(w_old[e], z);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (16 * i + c < lo) x[i][e] = z[i] * s_old;
       }
     }
   }
-  if (keys) {
+  uint32_t w[8];
+  if (FMT == S4R_KV_INT8) {
+    float worst = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (keep >> (8 * i) & 0xFFu) continue;
-      uint2 w;
-      w.x = kv8_code4<FMT>(x[i][0], x[i][1], x[i][2], x[i][3], s, inv);
-      w.y = kv8_code4<FMT>(x[i][4], x[i][5], x[i][6], x[i][7], s, inv);
-      *reinterpret_cast<uint2*>(img + key_offset(16 * i + c, 8 * dc, DH)) = w;
+    for (int e = 0; e < 8; ++e) w[e] = kv8_int8x4(x[0][e], x[1][e], x[2][e], x[3][e], s, inv, worst);
+    if (!(worst < 0.5f * s)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = kv8_int8x4_exact(x[0][e], x[1][e], x[2][e], x[3][e], s, inv);
     }
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      uint32_t* p = reinterpret_cast<uint32_t*>(img + value_offset(c, 8 * dc + e));
-      uint32_t w = kv8_code4<FMT>(x[0][e], x[1][e], x[2][e], x[3][e], s, inv);
-      if (keep) w = (w & ~keep) | (*p & keep);
-      *p = w;
-    }
+    for (int e = 0; e < 8; ++e) w[e] = kv8_e4m3x4(x[0][e], x[1][e], x[2][e], x[3][e], inv);
   }
-  __syncthreads();
+  if (inv == 0.f) {                                            // a block of zeros, or one that holds no values
 #pragma unroll
-  for (int i = 0; i < 2; ++i) reinterpret_cast<uint4*>(codes)[t + i * NT] = reinterpret_cast<const uint4*>(img)[t + i * NT];
+    for (int e = 0; e < 8; ++e) w[e] = 0;
+  }
+  if (!whole) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = (w[e] & ~keep) | (w_old[e] & keep);
+  }
+  put_codes<DH>(img, keys, c, dc, w);
+  __syncthreads();
+  codes[0] = image[0];
+  codes[NT] = image[NT];
   if (t == 0) *scale = s;
 }
 
@@ -174,44 +210,45 @@ __global__ __launch_bounds__(DH * 2) void k_kv8_read(const uint8_t* __restrict__
                                                      const float* __restrict__ v_scales,
                                                      const int32_t* __restrict__ starts,
                                                      const int32_t* __restrict__ counts, int64_t row0, int n_rows,
-                                                     int64_t cap, int tiles, T* __restrict__ k_out,
+                                                     int64_t cap, int tiles, int hkv, T* __restrict__ k_out,
                                                      T* __restrict__ v_out) {
   constexpr int NT = DH * 2;
-  const int j = blockIdx.y, b = blockIdx.z >> 1, hkv = gridDim.y;
-  const bool keys = (blockIdx.z & 1) == 0;
+  const Place at = place(hkv);
   const int t = threadIdx.x, c = t / (DH / 8), dc = t % (DH / 8);
   int64_t start;
   int count;
-  kv8_rows(starts, counts, b, row0, n_rows, cap, start, count);
-  const int64_t tile = start / kKv8Block + blockIdx.x;
+  kv8_rows(starts, counts, at.b, row0, n_rows, cap, start, count);
+  const int64_t tile = start / kKv8Block + at.blk;
   const int64_t first = tile * kKv8Block - start;
   if (first >= n_rows) return;
-  float x[4][8];
+  __shared__ __align__(16) uint8_t img[kKv8Block * DH];
+  kv8_u4* image = reinterpret_cast<kv8_u4*>(img) + t;
+  float s = 0.f;
   if (first < count) {
-    const int64_t at = ((int64_t)b * hkv + j) * tiles + tile;
-    const uint8_t* codes = (keys ? k_codes : v_codes) + at * (kKv8Block * DH);
-    const float s = (keys ? k_scales : v_scales)[at];
-    __shared__ __align__(16) uint8_t img[kKv8Block * DH];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      reinterpret_cast<uint4*>(img)[t + i * NT] = reinterpret_cast<const uint4*>(codes)[t + i * NT];
-    __syncthreads();
-    pieces_of<FMT, DH>(img, keys, c, dc, x);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[i][e] *= s;
+    const int64_t blk = ((int64_t)at.b * hkv + at.j) * tiles + tile;
+    const kv8_u4* codes = reinterpret_cast<const kv8_u4*>((at.keys ? k_codes : v_codes) + blk * (kKv8Block * DH)) + t;
+    const kv8_u4 a = codes[0], b = codes[NT];
+    s = (at.keys ? k_scales : v_scales)[blk];
+    image[0] = a;
+    image[NT] = b;
   }
-  T* out = (keys ? k_out : v_out) + (int64_t)b * n_rows * hkv * DH + (int64_t)j * DH + 8 * dc;
+  __syncthreads();
+  uint32_t w[8];
+  get_codes<DH>(img, at.keys, c, dc, w);
+  float x[4][8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float z[4];
+    kv8_numbers<FMT>(w[e], z);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i][e] = 16 * i + c < count - first ? z[i] * s : 0.f;
+  }
+  const int64_t width = (int64_t)hkv * DH;
+  T* out = (at.keys ? k_out : v_out) + ((int64_t)at.b * n_rows + first) * width + (int64_t)at.j * DH + 8 * dc;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int64_t r = first + 16 * i + c;
-    if (r < 0 || r >= n_rows) continue;
-    if (r >= count) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[i][e] = 0.f;
-    }
-    store8(out + r * hkv * DH, x[i]);
+    if (r >= 0 && r < n_rows) store8(out + (16 * i + c) * width, x[i]);
   }
 }
 
@@ -249,9 +286,9 @@ hipError_t launch_kv8_write(const Problem& P, const Kv8& C, int64_t n_rows, cons
                             const void* v_rows, int64_t v_stride, hipStream_t st) {
   by_type(P, C.format, [&](auto elem, auto fmt, auto dh) {
     using T = decltype(elem);
-    hipLaunchKernelGGL((k_kv8_write<T, fmt(), dh()>), dim3(blocks_touched(C, n_rows), P.hkv, 2 * P.B), dim3(2 * dh()),
-                       0, st, (const T*)k_rows, k_stride, (const T*)v_rows, v_stride, C.k_codes, C.k_scales, C.v_codes,
-                       C.v_scales, C.starts, C.counts, C.row0, (int)n_rows, P.cap, kv8_tiles(P));
+    hipLaunchKernelGGL((k_kv8_write<T, fmt(), dh()>), dim3(blocks_touched(C, n_rows) * P.hkv, 2, P.B),
+                       dim3(2 * dh()), 0, st, (const T*)k_rows, k_stride, (const T*)v_rows, v_stride, C.k_codes, C.k_scales, C.v_codes,
+                       C.v_scales, C.starts, C.counts, C.row0, (int)n_rows, P.cap, kv8_tiles(P), P.hkv);
   });
   return hipGetLastError();
 }
@@ -259,9 +296,9 @@ hipError_t launch_kv8_write(const Problem& P, const Kv8& C, int64_t n_rows, cons
 hipError_t launch_kv8_read(const Problem& P, const Kv8& C, int64_t n_rows, void* k_out, void* v_out, hipStream_t st) {
   by_type(P, C.format, [&](auto elem, auto fmt, auto dh) {
     using T = decltype(elem);
-    hipLaunchKernelGGL((k_kv8_read<T, fmt(), dh()>), dim3(blocks_touched(C, n_rows), P.hkv, 2 * P.B), dim3(2 * dh()), 0,
-                       st, C.k_codes, C.k_scales, C.v_codes, C.v_scales, C.starts, C.counts, C.row0, (int)n_rows, P.cap,
-                       kv8_tiles(P), (T*)k_out, (T*)v_out);
+    hipLaunchKernelGGL((k_kv8_read<T, fmt(), dh()>), dim3(blocks_touched(C, n_rows) * P.hkv, 2, P.B),
+                       dim3(2 * dh()), 0, st, C.k_codes, C.k_scales, C.v_codes, C.v_scales, C.starts, C.counts, C.row0, (int)n_rows, P.cap,
+                       kv8_tiles(P), P.hkv, (T*)k_out, (T*)v_out);
   });
   return hipGetLastError();
 }
