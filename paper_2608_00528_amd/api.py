@@ -403,22 +403,38 @@ def dense_decode(cfg, n_tokens, q, k_cache, v_cache, ws, out=None):
     return out
 
 
-def _here(t, name):
+def _device():
+    """The current device's index; None without a GPU, where no tensor argument passes its checks."""
+    try:
+        return torch.cuda.current_device()
+    except (RuntimeError, AssertionError):
+        return None
+
+
+def _here(t, name, dev):
     """The tensor's device has to be the current one: the launch goes to its stream."""
-    if t is not None and t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, not on the current device {torch.cuda.current_device()}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not on the current device {dev}")
 
 
-def _rows(t, name, dtype, width):
+def _rows(t, name, dtype, width, dev):
     """(address, rows, elements between rows) of a GPU tensor [..., heads, head_dim] or [..., width] whose last
     axes are packed to rows of `width` and whose leading axes step evenly from row to row."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    _here(t, name)
-    shape, strides = t.shape, t.stride()
-    d, n = len(shape), 1
+    _here(t, name, dev)
+    shape = t.shape
+    d = len(shape)
+    # the usual cases first: a packed tensor, one leading axis
+    if d > 1:
+        lead = d - 1 if shape[-1] == width else d - 2
+        if lead == d - 1 or shape[-1] * shape[-2] == width:
+            n = t.numel()
+            if n and t.is_contiguous():
+                return t.data_ptr(), n // width, width
+    strides, n = t.stride(), 1
     while d and n < width:
         d -= 1
         if strides[d] != n and shape[d] != 1:
@@ -439,11 +455,11 @@ def _rows(t, name, dtype, width):
     return t.data_ptr(), rows, width if stride is None else stride
 
 
-def _ints(t, name, n):
+def _ints(t, name, n, dev):
     if t is None:
         return None
     p = _ptr(t, name, torch.int32)
-    _here(t, name)
+    _here(t, name, dev)
     if t.numel() != n:
         raise ValueError(f"{name} has {t.numel()} entries, expected {n}")
     return p
@@ -455,39 +471,42 @@ def qk_norm_rope(cfg, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, q
     (int32, one per token; rope_theta = 0: not rotated, positions may be None).  q or k may be None.  The tokens may
     be slices of a fused projection's rows; outputs (new packed tensors by default) may be the inputs themselves.
     Returns (q_out, k_out)."""
-    dt = storage_dtype(cfg)
-    dh, n = cfg.head_dim, None
+    dt, dh, dev, n = storage_dtype(cfg), cfg.head_dim, _device(), None
     args, outs = [], []
     for name, x, o, heads in (("q", q, q_out, cfg.n_q_heads), ("k", k, k_out, cfg.n_kv_heads)):
         if x is None:
             if o is not None:
                 raise ValueError(f"{name}_out without {name}")
-            args += [None, 0, None, 0]
+            args += (None, 0, None, 0)
             outs.append(None)
             continue
-        p, rows, stride = _rows(x, name, dt, heads * dh)
+        p, rows, stride = _rows(x, name, dt, heads * dh, dev)
         if n is not None and rows != n:
             raise ValueError(f"q has {n} tokens and k {rows}")
         n = rows
         if o is None:
-            o = torch.empty(x.shape, dtype=dt, device=x.device)
-        po, ro, so = _rows(o, name + "_out", dt, heads * dh)
-        if ro != n:
-            raise ValueError(f"{name}_out has {ro} tokens, expected {n}")
-        args += [p, stride, po, so]
+            o = x.new_empty(x.shape)
+            args += (p, stride, o.data_ptr(), heads * dh)
+        else:
+            po, ro, so = _rows(o, name + "_out", dt, heads * dh, dev)
+            if ro != n:
+                raise ValueError(f"{name}_out has {ro} tokens, expected {n}")
+            args += (p, stride, po, so)
         outs.append(o)
     if n is None:
         raise ValueError("q or k is required")
-    _apart(args, n, cfg, dt)
+    if q_out is not None or k_out is not None:
+        _apart(args, n, cfg, dt)
+    weights = []
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        weights.append(_ptr(w, name, dt, False))
         if w is not None:
-            _here(w, name)
+            _here(w, name, dev)
             if w.numel() != dh:
                 raise ValueError(f"{name} has {w.numel()} entries, expected {dh}")
     L.check(L.load().s4r_qk_norm_rope(
-        _cfgp(cfg), n, args[0], args[1], args[4], args[5], _ptr(q_weight, "q_weight", dt, False),
-        _ptr(k_weight, "k_weight", dt, False), eps, _ints(positions, "positions", n), args[2], args[3], args[6],
-        args[7], _stream()))
+        _cfgp(cfg), n, args[0], args[1], args[4], args[5], weights[0], weights[1], eps,
+        _ints(positions, "positions", n, dev), args[2], args[3], args[6], args[7], _stream()))
     return tuple(outs)
 
 
@@ -523,7 +542,7 @@ class KV8Cache:
     """The tensors of an 8-bit KV cache (kv8_alloc): codes [B, h_kv, T, 64 d_h] uint8 and scales [B, h_kv, T]
     fp32 of both sides, T = ceil(capacity / 64); format "int8" or "e4m3"."""
 
-    __slots__ = ("format", "k_codes", "k_scales", "v_codes", "v_scales", "_c")
+    __slots__ = ("format", "k_codes", "k_scales", "v_codes", "v_scales", "_c", "_sizes", "_devices")
 
     def __init__(self, format, k_codes, k_scales, v_codes, v_scales):
         if format not in _KV_FORMATS:
@@ -533,6 +552,8 @@ class KV8Cache:
         self._c = L.KV8(_KV_FORMATS[format], _ptr(k_codes, "k_codes", torch.uint8),
                         _ptr(k_scales, "k_scales", torch.float32), _ptr(v_codes, "v_codes", torch.uint8),
                         _ptr(v_scales, "v_scales", torch.float32))
+        self._sizes = (k_codes.numel(), k_scales.numel(), v_codes.numel(), v_scales.numel())
+        self._devices = {k_codes.get_device(), k_scales.get_device(), v_codes.get_device(), v_scales.get_device()}
 
 
 def kv8_size(cfg):
@@ -555,17 +576,17 @@ def kv8_alloc(cfg, format="int8", device="cuda"):
     return KV8Cache(format, *sides)
 
 
-def _kv8(cfg, cache):
+def _kv8(cfg, cache, dev):
     """The C view of a cache, its tensors' sizes checked against cfg."""
     if not isinstance(cache, KV8Cache):
         raise ValueError("cache must be a KV8Cache")
     blocks = cfg.batch * cfg.n_kv_heads * ((cfg.capacity + L.KV8_BLOCK - 1) // L.KV8_BLOCK)
-    for name, n in (("k_codes", blocks * L.KV8_BLOCK * cfg.head_dim), ("k_scales", blocks),
-                    ("v_codes", blocks * L.KV8_BLOCK * cfg.head_dim), ("v_scales", blocks)):
-        t = getattr(cache, name)
-        if t.numel() != n:
-            raise ValueError(f"{name} has {t.numel()} elements, expected {n}")
-        _here(t, name)
+    codes = blocks * L.KV8_BLOCK * cfg.head_dim
+    if cache._sizes != (codes, blocks, codes, blocks):
+        raise ValueError(f"the cache's codes and scales have {cache._sizes} elements, expected {codes} and {blocks} "
+                         "for each side")
+    if cache._devices != {dev}:
+        raise ValueError(f"the cache is on {cache.k_codes.device}, not on the current device {dev}")
     return ctypes.byref(cache._c)
 
 
@@ -574,33 +595,36 @@ def kv8_write(cfg, cache, k, v, row0=0, starts=None, counts=None):
     starts[b] + i (int32 GPU tensor; row0 + i without it) for i < counts[b] (all without it).  A sequence whose range
     does not fit is left as it is."""
     dt, width = storage_dtype(cfg), cfg.n_kv_heads * cfg.head_dim
-    c = _kv8(cfg, cache)
-    pk, rows, sk = _rows(k, "k", dt, width)
-    pv, rv, sv = _rows(v, "v", dt, width)
+    dev = _device()
+    c = _kv8(cfg, cache, dev)
+    pk, rows, sk = _rows(k, "k", dt, width, dev)
+    pv, rv, sv = _rows(v, "v", dt, width, dev)
     if rows != rv or rows % cfg.batch:
         raise ValueError(f"k has {rows} rows and v {rv}: a multiple of the batch {cfg.batch}, the same for both, "
                          "was expected")
-    L.check(L.load().s4r_kv8_write(_cfgp(cfg), c, rows // cfg.batch, row0, _ints(starts, "starts", cfg.batch),
-                                   _ints(counts, "counts", cfg.batch), pk, sk, pv, sv, _stream()))
+    L.check(L.load().s4r_kv8_write(_cfgp(cfg), c, rows // cfg.batch, row0, _ints(starts, "starts", cfg.batch, dev),
+                                   _ints(counts, "counts", cfg.batch, dev), pk, sk, pv, sv, _stream()))
 
 
 def kv8_read(cfg, cache, n_rows, row0=0, starts=None, counts=None, k=None, v=None):
     """The tokens starts[b] + i (row0 + i), i < n_rows, of every sequence in the storage dtype: (k, v)
     [B, n_rows, h_kv d_h].  Rows from counts[b] on are zeros."""
     dt = storage_dtype(cfg)
-    c = _kv8(cfg, cache)
-    shape = (cfg.batch, n_rows, cfg.n_kv_heads * cfg.head_dim)
+    dev = _device()
+    c = _kv8(cfg, cache, dev)
+    shape = (cfg.batch, max(n_rows, 0), cfg.n_kv_heads * cfg.head_dim)
     out = []
     for name, t in (("k", k), ("v", v)):
         if t is None:
             t = torch.empty(shape, dtype=dt, device=cache.k_codes.device)
         elif t.numel() != shape[0] * shape[1] * shape[2]:
             raise ValueError(f"{name} has {t.numel()} elements, expected {shape}")
-        _here(t, name)
         out.append(t)
-    L.check(L.load().s4r_kv8_read(_cfgp(cfg), c, n_rows, row0, _ints(starts, "starts", cfg.batch),
-                                  _ints(counts, "counts", cfg.batch), _ptr(out[0], "k", dt), _ptr(out[1], "v", dt),
-                                  _stream()))
+    ptrs = [_ptr(t, name, dt) for t, name in zip(out, "kv")]
+    for t, name in zip(out, "kv"):
+        _here(t, name, dev)
+    L.check(L.load().s4r_kv8_read(_cfgp(cfg), c, n_rows, row0, _ints(starts, "starts", cfg.batch, dev),
+                                  _ints(counts, "counts", cfg.batch, dev), ptrs[0], ptrs[1], _stream()))
     return tuple(out)
 
 
@@ -620,21 +644,22 @@ def kv8_decode(cfg, cache, n_tokens, q, ws, lengths=None, out=None):
     n_tokens are used).  Query token i of n sees all but the newest n - 1 - i tokens.  ws: alloc_kv8_workspace.
     Returns fp32 of q's shape."""
     dt = storage_dtype(cfg)
-    c = _kv8(cfg, cache)
+    dev = _device()
+    c = _kv8(cfg, cache, dev)
     per = cfg.batch * cfg.n_q_heads * cfg.head_dim
     p = _ptr(q, "q", dt)
-    _here(q, "q")
+    _here(q, "q", dev)
     if q.numel() == 0 or q.numel() % per:
         raise ValueError(f"q has shape {tuple(q.shape)}: [batch, n, n_q_heads, head_dim] was expected")
     if out is None:
         out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
     elif out.numel() != q.numel():
         raise ValueError(f"out has {out.numel()} elements, expected {q.numel()}")
-    _here(out, "out")
-    _here(ws, "ws")
-    L.check(L.load().s4r_kv8_decode(_cfgp(cfg), c, n_tokens, _ints(lengths, "lengths", cfg.batch), q.numel() // per, p,
-                                    _ptr(out, "out", torch.float32), _ptr(ws, "ws", torch.uint8), ws.numel(),
-                                    _stream()))
+    po, pw = _ptr(out, "out", torch.float32), _ptr(ws, "ws", torch.uint8)
+    _here(out, "out", dev)
+    _here(ws, "ws", dev)
+    L.check(L.load().s4r_kv8_decode(_cfgp(cfg), c, n_tokens, _ints(lengths, "lengths", cfg.batch, dev), q.numel() // per, p,
+                                    po, pw, ws.numel(), _stream()))
     return out
 
 

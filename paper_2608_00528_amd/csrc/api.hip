@@ -496,7 +496,7 @@ s4r_status make_kv8(const Problem& P, const s4r_kv8* cache, Kv8& C) {
   if ((int64_t)P.hkv * (kv8_tiles(P) + 1) > UINT32_MAX / (2 * 128))
     return fail(S4R_ERR_UNSUPPORTED, "%lld blocks per sequence and side are too many",
                 (long long)P.hkv * kv8_tiles(P));
-  if ((int64_t)P.B * P.hkv * kv8_tiles(P) > INT32_MAX / 2)
+  if ((int64_t)P.B * P.hkv * (kv8_tiles(P) + 8) > INT32_MAX / 2)
     return fail(S4R_ERR_UNSUPPORTED, "a cache of %lld blocks per side is too large",
                 (long long)P.B * P.hkv * kv8_tiles(P));
   C = Kv8{cache->format, (uint8_t*)cache->k_codes, cache->k_scales, (uint8_t*)cache->v_codes, cache->v_scales,

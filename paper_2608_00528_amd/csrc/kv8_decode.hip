@@ -29,6 +29,7 @@ namespace s4r {
 namespace {
 
 constexpr int kWaves = 4;
+constexpr int kPairBlocks = 16;
 constexpr float kGrow = 6.f;            // the running maximum follows once a logit is 2^6 above it
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -79,60 +80,87 @@ struct Seqs {
 };
 __device__ __forceinline__ int blocks_of(int tokens) { return (tokens + kKv8Block - 1) / kKv8Block; }
 __device__ __forceinline__ int wave_scan(int x) {               // inclusive prefix sum over the lanes
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    const int y = __shfl_up(x, m);
-    if (lane >= m) x += y;
-  }
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);   // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);   // row_bcast:31 into rows 2 and 3
   return x;
 }
-// blocks of all (sequence, KV head) pairs; every wave computes the same
-__device__ __forceinline__ int all_blocks(const Seqs& S) {
-  if (!S.lengths) return S.B * S.hkv * blocks_of(S.n_max);
-  int n = 0;
-  for (int b0 = 0; b0 < S.B; b0 += 64) {
-    const int b = b0 + (int)(threadIdx.x & 63);
-    n += __shfl(wave_scan(b < S.B ? blocks_of(S.tokens(b)) * S.hkv : 0), 63);
-  }
-  return n;
+
+// The (sequence, KV head) pairs lie on a line that is cut into equal runs.  A pair takes
+// its blocks rounded up to one for every wave, and room for another round where it is
+// shorter than a run: ending a pair costs a run about as much (2.4 us), and a run of
+// many short pairs would end long after the others.
+__host__ __device__ inline int pair_length(int blocks, int shorter) {
+  return blocks == 0 ? 0 : (blocks + kWaves - 1) / kWaves * kWaves + (blocks < shorter ? kWaves : 0);
 }
-// blocks of one workgroup's run: a multiple of the waves
-__device__ __forceinline__ int run_of(int total, int nwg) { return ((total + nwg - 1) / nwg + kWaves - 1) / kWaves * kWaves; }
-// the sequence that holds block u of them all, and its first block
-__device__ __forceinline__ void find_sequence(const Seqs& S, int u, int& seq, int& begin) {
-  if (!S.lengths) {
-    const int per = S.hkv * blocks_of(S.n_max);
-    seq = u / per;
-    begin = seq * per;
-    return;
-  }
-  int n = 0;
-  seq = begin = 0;
-  for (int b0 = 0; b0 < S.B; b0 += 64) {
+__host__ __device__ inline int run_length(int total, int nwg) {
+  return ((total + nwg - 1) / nwg + kWaves - 1) / kWaves * kWaves;
+}
+
+// the line; every wave holds the same, one sequence per lane, 64 at a time
+struct Order {
+  Seqs S;
+  int shorter;                // pairs of fewer blocks than this have the room
+  int base;                   // the lanes hold sequences base .. base + 63
+  int tok, mine, upto;        // this lane's sequence: tokens, its pairs' length, and the line up to its end
+  __device__ __forceinline__ explicit Order(const Seqs& s) : S(s), shorter(0) {}
+  __device__ __forceinline__ int length(int blocks) const { return pair_length(blocks, shorter); }
+  __device__ __forceinline__ void load(int b0, int before) {
     const int b = b0 + (int)(threadIdx.x & 63);
-    const int mine = b < S.B ? blocks_of(S.tokens(b)) * S.hkv : 0;
-    const int upto = n + wave_scan(mine);
-    const uint64_t past = __ballot(upto > u);
-    if (past) {
-      const int l = __ffsll((unsigned long long)past) - 1;
-      seq = b0 + l;
-      begin = __shfl(upto - mine, l);
+    base = b0;
+    tok = b < S.B ? S.tokens(b) : 0;
+    place(before);
+  }
+  __device__ __forceinline__ void place(int before) {
+    mine = length(blocks_of(tok)) * S.hkv;
+    upto = before + wave_scan(mine);
+  }
+  __device__ __forceinline__ int end() const { return __builtin_amdgcn_readlane(upto, 63); }
+  __device__ __forceinline__ int total() const {
+    if (S.B <= 64) return end();
+    if (!S.lengths) return S.B * S.hkv * length(blocks_of(S.n_max));
+    int n = 0;
+#pragma unroll 4
+    for (int b = threadIdx.x & 63; b < S.B; b += 64) n += length(blocks_of(S.tokens(b)));
+    return __builtin_amdgcn_readlane(wave_scan(n), 63) * S.hkv;
+  }
+  // the line laid out for nwg runs; returns the length of a run, a multiple of the waves
+  __device__ __forceinline__ int lay_out(int nwg) {
+    load(0, 0);
+    shorter = (total() + nwg - 1) / nwg;
+    place(0);
+    return run_length(total(), nwg);
+  }
+  // the sequence at u (the lanes move on to it): its number, place and tokens
+  __device__ __forceinline__ void find(int u, int& seq, int& begin, int& tokens) {
+    if (S.B > 64 && !S.lengths) {
+      const int per = length(blocks_of(S.n_max)) * S.hkv;
+      seq = u / per;
+      begin = seq * per;
+      tokens = S.n_max;
       return;
     }
-    n = __shfl(upto, 63);
+    while (end() <= u && base + 64 < S.B) load(base + 64, end());
+    const int l = __ffsll((unsigned long long)__ballot(upto > u)) - 1;
+    seq = base + l;
+    begin = __builtin_amdgcn_readlane(upto - mine, l);
+    tokens = __builtin_amdgcn_readlane(tok, l);
   }
-}
-// blocks before sequence b
-__device__ __forceinline__ int blocks_before(const Seqs& S, int b) {
-  if (!S.lengths) return b * S.hkv * blocks_of(S.n_max);
-  int n = 0;
-  for (int b0 = 0; b0 < b; b0 += 64) {
-    const int i = b0 + (int)(threadIdx.x & 63);
-    n += __shfl(wave_scan(i < b ? blocks_of(S.tokens(i)) * S.hkv : 0), 63);
+  // the place and tokens of sequence b
+  __device__ __forceinline__ void of(int b, int& begin, int& tokens) {
+    if (S.B > 64 && !S.lengths) {
+      begin = b * length(blocks_of(S.n_max)) * S.hkv;
+      tokens = S.n_max;
+      return;
+    }
+    while (base + 64 <= b) load(base + 64, end());
+    begin = __builtin_amdgcn_readlane(upto - mine, b & 63);
+    tokens = __builtin_amdgcn_readlane(tok, b & 63);
   }
-  return n;
-}
+};
 
 // query elements as bf16 parts: bf16 as stored, fp32 in three
 template <typename T>
@@ -163,7 +191,8 @@ template <typename T, int FMT, int DH>
 __global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
     const T* __restrict__ q, const uint8_t* __restrict__ k_codes, const float* __restrict__ k_scales,
     const uint8_t* __restrict__ v_codes, const float* __restrict__ v_scales, float* __restrict__ part_ml,
-    float* __restrict__ part_o, float* __restrict__ out, Seqs S, int nwg, int chunks, int n_q, int G, int tiles) {
+    float* __restrict__ part_o, float* __restrict__ out, Seqs S, int nwg, int by_pair, int chunks, int n_q, int G,
+    int tiles) {
   constexpr int NP = QParts<T>::n, NK = DH / 16, NV = DH / 16;   // 1 KiB pieces of a block per side
   constexpr int KB = DH / 64;
   // workgroups of one run's query chunks 8 ids apart: on one XCD, sharing its L2
@@ -172,9 +201,6 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 15, kg = lane >> 4;
   const int hkv = S.hkv, hq = hkv * G, rows = n_q * G;
-  const int total = __builtin_amdgcn_readfirstlane(all_blocks(S)), run = run_of(total, nwg);
-  const int u0 = w * run, u1 = min(u0 + run, total);
-
   __shared__ float wm[kWaves][kKv8Rows], wl[kWaves][kKv8Rows];
   __shared__ float wo[kWaves][kKv8Rows][DH];
 
@@ -182,42 +208,81 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
   const int back = row < rows ? n_q - 1 - row / G : 0;          // tokens that its query token does not see yet
   const float to_log2 = 1.4426950408889634f / sqrtf((float)DH);
 
-  for (int u = u0; u < u1;) {
-    int b, begin;
-    find_sequence(S, u, b, begin);
-    b = __builtin_amdgcn_readfirstlane(b);
-    begin = __builtin_amdgcn_readfirstlane(begin);
-    const int N = S.tokens(b), T_b = blocks_of(N);
-    const int j = (u - begin) / T_b, first = (u - begin) - j * T_b;
-    const int n = min(T_b - first, u1 - u);                     // blocks of this pair in this run
-    const int64_t at = ((int64_t)b * hkv + j) * tiles;
-    const u32x4* kp = reinterpret_cast<const u32x4*>(k_codes + at * (kKv8Block * DH)) + lane;
-    const u32x4* vp = reinterpret_cast<const u32x4*>(v_codes + at * (kKv8Block * DH)) + lane;
-    const float* ksp = k_scales + at;
-    const float* vsp = v_scales + at;
+  // a pair's blocks are [begin, end) of the line, the next pair begins at `next`;
+  // block0: its first block in the cache
+  struct Pair {
+    int b, j, N, begin, end, next, block0;
+  };
+  Order order(S);
+  auto pair_at = [&](int u) __attribute__((always_inline)) {
+    Pair p;
+    int begin;
+    order.find(u, p.b, begin, p.N);
+    const int blocks = blocks_of(p.N), length = order.length(blocks);
+    p.j = (u - begin) / length;
+    p.begin = begin + p.j * length;
+    p.end = p.begin + blocks;
+    p.next = p.begin + length;
+    p.block0 = (p.b * hkv + p.j) * tiles;
+    return p;
+  };
+  Pair pair, after;
+  int u0 = 0, u1;                                               // this workgroup's run
+  if (by_pair) {
+    pair.b = w / hkv;
+    pair.j = w - pair.b * hkv;
+    pair.N = __builtin_amdgcn_readfirstlane(S.tokens(pair.b));
+    pair.begin = 0;
+    u1 = pair.end = pair.next = blocks_of(pair.N);
+    pair.block0 = w * tiles;
+  } else {
+    const int run = order.lay_out(nwg);
+    u0 = w * run;
+    u1 = min(u0 + run, order.total());
+    if (u0 >= u1) return;
+    pair = pair_at(u0);
+  }
+  const u32x4* kp = reinterpret_cast<const u32x4*>(k_codes) + lane;
+  const u32x4* vp = reinterpret_cast<const u32x4*>(v_codes) + lane;
+  u32x4 kk[NK], vv[NV];
+  float sk, sv;
+  auto load_keys = [&](int block) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) kk[i] = __builtin_nontemporal_load(kp + (int64_t)block * (kKv8Block * DH / 16) + i * 64);
+    sk = k_scales[block];
+  };
+  auto load_values = [&](int block) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) vv[i] = __builtin_nontemporal_load(vp + (int64_t)block * (kKv8Block * DH / 16) + i * 64);
+    sv = v_scales[block];
+  };
 
-    u32x4 kk[NK], vv[NV];
-    float sk, sv;
-    auto load_keys = [&](int tile) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < NK; ++i) kk[i] = __builtin_nontemporal_load(kp + (int64_t)tile * (kKv8Block * DH / 16) + i * 64);
-      sk = ksp[tile];
-    };
-    auto load_values = [&](int tile) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) vv[i] = __builtin_nontemporal_load(vp + (int64_t)tile * (kKv8Block * DH / 16) + i * 64);
-      sv = vsp[tile];
-    };
+  // a wave takes every fourth block of the run, its next one on the way while it works
+  // on one, also where that lies in the next pair
+  int p = u0 + wave, have = -1;
+  if (p < min(pair.end, u1)) {
+    have = p;
+    load_keys(pair.block0 + p - pair.begin);
+    load_values(pair.block0 + p - pair.begin);
+  }
+  for (int us = u0;; us = after.begin, p = us + wave, pair = after) {
+    const int ue = min(pair.end, u1);
+    const bool more = pair.next < u1;
+    after = pair;
+    if (more) after = pair_at(pair.next);
+    const int pa0 = after.begin + wave;                         // this wave's first block there
+    const bool ahead = more && pa0 < min(after.end, u1);
+    const int b = pair.b, j = pair.j, N = pair.N;
     float M = -INFINITY, l = 0.f;
     floatx4 acc[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-    if (wave < n) {
-      int tile = first + wave;
-      const int last = first + wave + (n - 1 - wave) / kWaves * kWaves;
-      load_keys(tile);
-      load_values(tile);
+    if (p < ue) {
+      if (have != p) {
+        load_keys(pair.block0 + p - pair.begin);
+        load_values(pair.block0 + p - pair.begin);
+      }
       Op8 qb[KB][2][NP];
       {
         const int r = min(row, rows - 1);
@@ -227,7 +292,12 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
 #pragma unroll
           for (int h = 0; h < 2; ++h) QParts<T>::load(qp + d * 64 + 16 * kg + 8 * h, qb[d][h]);
       }
-      for (;; tile += kWaves) {
+      do {
+        const int tile = p - pair.begin;
+        // the wave's next block; behind the next pair, or the run: this one again
+        const bool on = p + kWaves < ue;
+        have = on ? p + kWaves : (ahead ? pa0 : -1);
+        const int block = on ? pair.block0 + tile + kWaves : (ahead ? after.block0 + wave : pair.block0 + tile);
         // logits
         floatx4 s[4];
 #pragma unroll
@@ -243,7 +313,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
             }
         }
         const float f = sk * to_log2;
-        load_keys(min(tile + kWaves, last));                    // past the end: the last one again
+        load_keys(block);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -326,9 +396,13 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
 #pragma unroll
             for (int p = 0; p < 3; ++p) acc[i] = mfma16x16x32(pa[h][p], bv, acc[i]);
           }
-        if (tile == last) break;
-        load_values(tile + kWaves);
-      }
+        load_values(block);
+        p += kWaves;
+      } while (p < ue);
+    }
+    if (!by_pair && us >= pair.end) {                           // the run begins in the room behind a pair
+      if (!more) break;
+      continue;
     }
     // merge the waves
     const float ls = rows_sum(l);
@@ -341,8 +415,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
 #pragma unroll
       for (int v = 0; v < 4; ++v) wo[wave][4 * kg + v][16 * i + col] = acc[i][v];
     __syncthreads();
-    const bool whole = first == 0 && n == T_b;
-    const int slot = first > 0 ? 2 * w : 2 * w + 1;
+    const bool whole = us == pair.begin && ue == pair.end;
+    const int slot = us > pair.begin ? 2 * w : 2 * w + 1;
     for (int e = t; e < kKv8Rows * DH; e += kWaves * 64) {
       const int r = e / DH, d = e % DH, gr = chunk * kKv8Rows + r;
       if (gr >= rows) break;
@@ -368,14 +442,14 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
         }
       }
     }
+    if (!more) break;
     __syncthreads();
-    u += n;
   }
 }
 
 // merges the partials of the pairs that runs cut, and writes the zeros of sequences
 // without tokens.  One workgroup per query row of a sequence, groups of DH / 4
-// threads over the partials.
+// threads over the partials, each with its own running maximum (one round of loads).
 template <int DH>
 __global__ __launch_bounds__(256) void k_kv8_combine(const float* __restrict__ part_ml, const float* __restrict__ part_o,
                                                      float* __restrict__ out, Seqs S, int nwg, int chunks, int n_q,
@@ -384,58 +458,68 @@ __global__ __launch_bounds__(256) void k_kv8_combine(const float* __restrict__ p
   const int gr = blockIdx.x, j = blockIdx.y, b = blockIdx.z;
   const int t = threadIdx.x, g = t / (DH / 4), d4 = t % (DH / 4);
   const int hq = S.hkv * G;
-  float4* dst = reinterpret_cast<float4*>(out + (((int64_t)b * n_q + gr / G) * hq + (int64_t)j * G + gr % G) * DH) + d4;
-  const int T_b = blocks_of(S.tokens(b));
+  float* dst = out + (((int64_t)b * n_q + gr / G) * hq + (int64_t)j * G + gr % G) * DH + 4 * d4;
+  Order order(S);
+  const int run = order.lay_out(nwg);
+  int begin, tokens;
+  order.of(b, begin, tokens);
+  const int T_b = blocks_of(tokens);
   if (T_b == 0) {
-    if (g == 0) *dst = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (g == 0) *reinterpret_cast<floatx4*>(dst) = floatx4{0.f, 0.f, 0.f, 0.f};
     return;
   }
-  const int run = run_of(all_blocks(S), nwg);
-  const int u0 = blocks_before(S, b) + j * T_b, u1 = u0 + T_b;
+  const int u0 = begin + j * order.length(T_b), u1 = u0 + T_b;
   const int w0 = u0 / run, w1 = (u1 - 1) / run;
   if (w0 == w1) return;                                         // finished by its run
   const int chunk = gr / kKv8Rows, row = gr % kKv8Rows;
-  auto slot = [&](int w) { return part_row(w == w0 ? 2 * w + 1 : 2 * w, chunks, chunk, row); };
-  float M = -INFINITY;
-  for (int w = w0 + t; w <= w1; w += 256) M = fmaxf(M, part_ml[slot(w) * 2]);
-  __shared__ float sm[4];
-  __shared__ float4 so[NG][DH / 4];
-  __shared__ float sl[NG];
-  M = wave_max(M);
-  if ((t & 63) == 0) sm[t >> 6] = M;
-  __syncthreads();
-  M = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
-  float l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float M = -INFINITY, l = 0.f;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
   for (int w = w0 + g; w <= w1; w += NG) {
-    const int64_t pr = slot(w);
+    const int64_t pr = part_row(w == w0 ? 2 * w + 1 : 2 * w, chunks, chunk, row);
     const float m = part_ml[pr * 2], pl = part_ml[pr * 2 + 1];
-    const float4 x = reinterpret_cast<const float4*>(part_o + pr * DH)[d4];
-    const float a = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - M);
-    l += a * pl;
-    o.x += a * x.x, o.y += a * x.y, o.z += a * x.z, o.w += a * x.w;
+    const floatx4 x = *reinterpret_cast<const floatx4*>(part_o + pr * DH + 4 * d4);
+    const float to = fmaxf(M, m);
+    // a partial without a maximum has sums of zero, or NaN, which stay
+    const float a = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(M - to);
+    const float c = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+    l = a * l + c * pl;
+    o = a * o + c * x;
+    M = to;
   }
+  __shared__ floatx4 so[NG][DH / 4];
+  __shared__ float sm[NG], sl[NG];
   so[g][d4] = o;
-  if (d4 == 0) sl[g] = l;
+  if (d4 == 0) {
+    sm[g] = M;
+    sl[g] = l;
+  }
   __syncthreads();
   if (g == 0) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) M = fmaxf(M, sm[i]);
     l = 0.f;
-    o = make_float4(0.f, 0.f, 0.f, 0.f);
+    o = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
-      l += sl[i];
-      const float4 x = so[i][d4];
-      o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
+      const float a = sm[i] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm[i] - M);
+      l += a * sl[i];
+      o += a * so[i][d4];
     }
     const float r = l == 0.f ? 0.f : 1.f / l;
-    *dst = make_float4(o.x * r, o.y * r, o.z * r, o.w * r);
+    *reinterpret_cast<floatx4*>(dst) = o * r;
   }
 }
 
 int row_chunks(const Problem& P, int n_q) { return (n_q * P.G + kKv8Rows - 1) / kKv8Rows; }
+// a workgroup for each pair where the caches are short: its waves take at most
+// kPairBlocks / 4 blocks each, and nothing is left to merge
+bool one_workgroup_per_pair(const Problem& P, int chunks, int64_t n_max) {
+  return n_max <= kPairBlocks * kKv8Block && (int64_t)P.B * P.hkv * chunks <= 1 << 23;   // workgroups of a grid
+}
 // runs of a call over at most n_max tokens per sequence: a block for every wave at least
 int runs(const Problem& P, int n_q, int64_t n_max) {
-  const int64_t blocks = (int64_t)P.B * P.hkv * ((n_max + kKv8Block - 1) / kKv8Block);
+  const int64_t blocks = (int64_t)P.B * P.hkv * pair_length((int)((n_max + kKv8Block - 1) / kKv8Block), 1 << 30);
   return (int)std::max<int64_t>(1, std::min<int64_t>((blocks + kWaves - 1) / kWaves, kKv8Wgs / row_chunks(P, n_q)));
 }
 
@@ -449,7 +533,9 @@ size_t kv8_ws_bytes(const Problem& P, int n_q) {
 
 hipError_t launch_kv8_decode(const Problem& P, const Kv8& C, int64_t n_max, const int32_t* lengths, int n_q,
                              const void* q, float* out, void* ws, hipStream_t st) {
-  const int nwg = runs(P, n_q, n_max), chunks = row_chunks(P, n_q);
+  const int chunks = row_chunks(P, n_q);
+  const bool by_pair = one_workgroup_per_pair(P, chunks, n_max);
+  const int nwg = by_pair ? P.B * P.hkv : runs(P, n_q, n_max);
   const size_t part_rows = (size_t)2 * nwg * chunks * kKv8Rows;
   float* part_o = (float*)ws;
   float* part_ml = part_o + part_rows * P.dh;
@@ -458,7 +544,7 @@ hipError_t launch_kv8_decode(const Problem& P, const Kv8& C, int64_t n_max, cons
   auto go = [&](auto elem, auto fmt, auto dh) {
     using T = decltype(elem);
     hipLaunchKernelGGL((k_kv8_decode<T, fmt(), dh()>), grid, dim3(kWaves * 64), 0, st, (const T*)q, C.k_codes, C.k_scales,
-                       C.v_codes, C.v_scales, part_ml, part_o, out, S, nwg, chunks, n_q, P.G, kv8_tiles(P));
+                       C.v_codes, C.v_scales, part_ml, part_o, out, S, nwg, (int)by_pair, chunks, n_q, P.G, kv8_tiles(P));
   };
   auto by_fmt = [&](auto elem, auto dh) {
     if (C.format == S4R_KV_INT8)
@@ -477,11 +563,13 @@ hipError_t launch_kv8_decode(const Problem& P, const Kv8& C, int64_t n_max, cons
   else
     by_type(std::integral_constant<int, 64>());
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  // no pair is cut where every run holds whole pairs of equal length
-  const int64_t per = (n_max + kKv8Block - 1) / kKv8Block, total = per * P.B * P.hkv;
-  const int64_t run = ((total + nwg - 1) / nwg + kWaves - 1) / kWaves * kWaves;
-  if (!lengths && run % per == 0) return hipSuccess;
+  if (e != hipSuccess || by_pair) return e;
+  // sequences of one length: no pair is cut where the runs hold whole ones
+  if (!lengths) {
+    const int blocks = (int)((n_max + kKv8Block - 1) / kKv8Block), pairs = P.B * P.hkv;
+    const int length = pair_length(blocks, (pair_length(blocks, 0) * pairs + nwg - 1) / nwg);
+    if (run_length(length * pairs, nwg) % length == 0) return hipSuccess;
+  }
   const dim3 cgrid(n_q * P.G, P.hkv, P.B);
   if (P.dh == 128)
     hipLaunchKernelGGL(k_kv8_combine<128>, cgrid, dim3(256), 0, st, part_ml, part_o, out, S, nwg, chunks, n_q, P.G);

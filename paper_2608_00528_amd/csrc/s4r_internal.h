@@ -118,7 +118,7 @@ inline double rope_ratio(const Problem& P) { return P.theta == 0.f ? 0.0 : pow((
 constexpr int kKv8Block = 64;         // tokens per block (one scale per side and KV head)
 constexpr int kKv8Rows = 16;          // query rows (query token x group member) per attention workgroup
 constexpr int kKv8MaxRows = 128;      // n_q * G
-constexpr int kKv8Wgs = 512;          // attention workgroups: two per CU
+constexpr int kKv8Wgs = 256;          // attention workgroups: one per CU
 struct Kv8 {
   int format;                         // S4R_KV_INT8 | S4R_KV_E4M3
   uint8_t* k_codes;                   // [B][hkv][tiles][64 * dh]
