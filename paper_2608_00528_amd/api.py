@@ -542,18 +542,13 @@ class KV8Cache:
     """The tensors of an 8-bit KV cache (kv8_alloc): codes [B, h_kv, T, 64 d_h] uint8 and scales [B, h_kv, T]
     fp32 of both sides, T = ceil(capacity / 64); format "int8" or "e4m3"."""
 
-    __slots__ = ("format", "k_codes", "k_scales", "v_codes", "v_scales", "_c", "_sizes", "_devices")
+    __slots__ = ("format", "k_codes", "k_scales", "v_codes", "v_scales")
 
     def __init__(self, format, k_codes, k_scales, v_codes, v_scales):
         if format not in _KV_FORMATS:
             raise ValueError(f"format {format!r}: one of {sorted(_KV_FORMATS)} was expected")
         self.format = format
         self.k_codes, self.k_scales, self.v_codes, self.v_scales = k_codes, k_scales, v_codes, v_scales
-        self._c = L.KV8(_KV_FORMATS[format], _ptr(k_codes, "k_codes", torch.uint8),
-                        _ptr(k_scales, "k_scales", torch.float32), _ptr(v_codes, "v_codes", torch.uint8),
-                        _ptr(v_scales, "v_scales", torch.float32))
-        self._sizes = (k_codes.numel(), k_scales.numel(), v_codes.numel(), v_scales.numel())
-        self._devices = {k_codes.get_device(), k_scales.get_device(), v_codes.get_device(), v_scales.get_device()}
 
 
 def kv8_size(cfg):
@@ -568,6 +563,8 @@ def kv8_alloc(cfg, format="int8", device="cuda"):
     if format not in _KV_FORMATS:
         raise ValueError(f"format {format!r}: one of {sorted(_KV_FORMATS)} was expected")
     kv8_size(cfg)                                    # the library's own checks of cfg
+    if torch.device(device).type != "cuda":
+        raise ValueError(f"device {device}: a GPU was expected")
     shape = (cfg.batch, cfg.n_kv_heads, (cfg.capacity + L.KV8_BLOCK - 1) // L.KV8_BLOCK)
     sides = []
     for _ in range(2):
@@ -577,17 +574,21 @@ def kv8_alloc(cfg, format="int8", device="cuda"):
 
 
 def _kv8(cfg, cache, dev):
-    """The C view of a cache, its tensors' sizes checked against cfg."""
+    """The C view of a cache, its tensors checked against cfg."""
     if not isinstance(cache, KV8Cache):
         raise ValueError("cache must be a KV8Cache")
     blocks = cfg.batch * cfg.n_kv_heads * ((cfg.capacity + L.KV8_BLOCK - 1) // L.KV8_BLOCK)
     codes = blocks * L.KV8_BLOCK * cfg.head_dim
-    if cache._sizes != (codes, blocks, codes, blocks):
-        raise ValueError(f"the cache's codes and scales have {cache._sizes} elements, expected {codes} and {blocks} "
-                         "for each side")
-    if cache._devices != {dev}:
-        raise ValueError(f"the cache is on {cache.k_codes.device}, not on the current device {dev}")
-    return ctypes.byref(cache._c)
+    view = [_KV_FORMATS[cache.format]]
+    for name, t, dt, n in (("k_codes", cache.k_codes, torch.uint8, codes),
+                           ("k_scales", cache.k_scales, torch.float32, blocks),
+                           ("v_codes", cache.v_codes, torch.uint8, codes),
+                           ("v_scales", cache.v_scales, torch.float32, blocks)):
+        view.append(_ptr(t, name, dt))
+        if t.numel() != n:
+            raise ValueError(f"{name} has {t.numel()} elements, expected {n}")
+        _here(t, name, dev)
+    return ctypes.byref(L.KV8(*view))
 
 
 def kv8_write(cfg, cache, k, v, row0=0, starts=None, counts=None):
@@ -616,7 +617,7 @@ def kv8_read(cfg, cache, n_rows, row0=0, starts=None, counts=None, k=None, v=Non
     out = []
     for name, t in (("k", k), ("v", v)):
         if t is None:
-            t = torch.empty(shape, dtype=dt, device=cache.k_codes.device)
+            t = cache.k_codes.new_empty(shape, dtype=dt)
         elif t.numel() != shape[0] * shape[1] * shape[2]:
             raise ValueError(f"{name} has {t.numel()} elements, expected {shape}")
         out.append(t)
@@ -652,7 +653,7 @@ def kv8_decode(cfg, cache, n_tokens, q, ws, lengths=None, out=None):
     if q.numel() == 0 or q.numel() % per:
         raise ValueError(f"q has shape {tuple(q.shape)}: [batch, n, n_q_heads, head_dim] was expected")
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        out = q.new_empty(q.shape, dtype=torch.float32)
     elif out.numel() != q.numel():
         raise ValueError(f"out has {out.numel()} elements, expected {q.numel()}")
     po, pw = _ptr(out, "out", torch.float32), _ptr(ws, "ws", torch.uint8)
