@@ -188,7 +188,7 @@ __device__ __forceinline__ int64_t part_row(int slot, int chunks, int chunk, int
 }
 
 template <typename T, int FMT, int DH>
-__global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 || DH == 64 ? 2 : 1) void k_kv8_decode(
     const T* __restrict__ q, const uint8_t* __restrict__ k_codes, const float* __restrict__ k_scales,
     const uint8_t* __restrict__ v_codes, const float* __restrict__ v_scales, float* __restrict__ part_ml,
     float* __restrict__ part_o, float* __restrict__ out, Seqs S, int nwg, int by_pair, int chunks, int n_q, int G,
@@ -301,17 +301,20 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
         // logits
         floatx4 s[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 4; ++i) s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+        // four sums side by side: a sum's next product waits for the one before it
 #pragma unroll
-          for (int d = 0; d < KB; ++d)
+        for (int d = 0; d < KB; ++d)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const Op8 a = codes_to_bf16<FMT>(kk[i * KB + d][2 * h], kk[i * KB + d][2 * h + 1]);
+          for (int h = 0; h < 2; ++h) {
+            Op8 a[4];
 #pragma unroll
-              for (int p = 0; p < NP; ++p) s[i] = mfma16x16x32(a, qb[d][h][p], s[i]);
-            }
-        }
+            for (int i = 0; i < 4; ++i) a[i] = codes_to_bf16<FMT>(kk[i * KB + d][2 * h], kk[i * KB + d][2 * h + 1]);
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[i] = mfma16x16x32(a[i], qb[d][h][p], s[i]);
+          }
         const float f = sk * to_log2;
         load_keys(block);
 #pragma unroll
@@ -389,12 +392,16 @@ __global__ __launch_bounds__(kWaves * 64, 2) void k_kv8_decode(
             pa[h][p].u = make_uint4(o[0], o[1], o[2], o[3]);
           }
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i0 = 0; i0 < NV; i0 += 4)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const Op8 bv = codes_to_bf16<FMT>(vv[i][2 * h], vv[i][2 * h + 1]);
+            Op8 bv[4];
 #pragma unroll
-            for (int p = 0; p < 3; ++p) acc[i] = mfma16x16x32(pa[h][p], bv, acc[i]);
+            for (int i = 0; i < 4; ++i) bv[i] = codes_to_bf16<FMT>(vv[i0 + i][2 * h], vv[i0 + i][2 * h + 1]);
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[i0 + i] = mfma16x16x32(pa[h][p], bv[i], acc[i0 + i]);
           }
         load_values(block);
         p += kWaves;
