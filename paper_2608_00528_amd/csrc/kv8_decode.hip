@@ -350,15 +350,16 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 || DH == 64 ? 2 : 1) vo
           }
         }
         const float ref = M == -INFINITY ? 0.f : M;
-        float x[4][4];
+        float x[4][4], sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             const float p = __builtin_amdgcn_exp2f(s[i][v] - ref);
-            l += p;
+            sum += p;
             x[i][v] = p * sv;
           }
+        l += sum;
         if (part) {
           // a token that is not seen takes no part, whatever its block's scale or codes are
 #pragma unroll
@@ -391,8 +392,13 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 || DH == 64 ? 2 : 1) vo
             }
             pa[h][p].u = make_uint4(o[0], o[1], o[2], o[3]);
           }
+        // a block's products from zero, then added: the matrix unit cuts what it adds to a
+        // large sum, which over a run of 64 blocks had made 2.3e-6 of the result
 #pragma unroll
-        for (int i0 = 0; i0 < NV; i0 += 4)
+        for (int i0 = 0; i0 < NV; i0 += 4) {
+          floatx4 o[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             Op8 bv[4];
@@ -401,8 +407,11 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 || DH == 64 ? 2 : 1) vo
 #pragma unroll
             for (int p = 0; p < 3; ++p)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) acc[i0 + i] = mfma16x16x32(pa[h][p], bv[i], acc[i0 + i]);
+              for (int i = 0; i < 4; ++i) o[i] = mfma16x16x32(pa[h][p], bv[i], o[i]);
           }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[i0 + i] += o[i];
+        }
         load_values(block);
         p += kWaves;
       } while (p < ue);
