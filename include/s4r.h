@@ -493,8 +493,9 @@ s4r_status s4r_kv8_read(const s4r_config* cfg, const s4r_kv8* cache, int64_t n_r
  * as sequences grow up to N.  A query token that sees nothing gets zeros.  Query
  * elements must be finite.  1 <= N <= capacity, 1 <= n_q and n_q * G <= 128.
  * ws: s4r_kv8_workspace_size bytes, 256-byte aligned; its contents do not matter.
- * Scores and sums are fp32; the 8-bit codes and bf16 queries enter the matrix cores
- * exactly, the weights (and fp32 queries) as three bf16 parts, 24 bits.
+ * Sums are fp32.  The codes enter the matrix cores exactly, and so do the elements of
+ * a bf16 query row down to 2^-28 of its largest; fp32 queries and the softmax weights
+ * enter with 22 bits.
  */
 s4r_status s4r_kv8_workspace_size(const s4r_config* cfg, int32_t n_q, size_t* bytes);
 s4r_status s4r_kv8_decode(const s4r_config* cfg, const s4r_kv8* cache, int64_t N, const int32_t* lengths,

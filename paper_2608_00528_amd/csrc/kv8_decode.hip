@@ -8,14 +8,17 @@
 // 2 d_h bytes per token and KV head, so every other cost has to hide under the
 // stream:
 //  - the codes are operands as loaded (16 bytes per lane, 1 KiB per wave load) and
-//    become bf16 exactly; 16 query rows (query token x group member) share them;
+//    become fp16 exactly; 16 or 32 query rows (query token x group member) share them;
 //  - logits as K q^T: 16 tokens x 16 query rows per MFMA, so lane l ends with
 //    query row l % 16 and the tokens 16 i + 4 (l / 16) + v of the block - which is
 //    the A operand of P V, with no exchange between lanes;
 //  - scales are one number per block: the logits' goes into the exponent's factor,
-//    the values' into p;
-//  - p keeps 24 bits as three bf16 parts (a truncated part of each remainder), so
-//    the products with the 8-bit codes are exact and sums are fp32.
+//    the values' into the addition of the block's sums;
+//  - a query row is scaled by a power of two to just below 2^15, where bf16 elements
+//    are fp16 numbers (exactly, down to 2^-28 of the row's largest) and fp32 ones two
+//    fp16 parts (22 bits); weights are kept at 2^9 to 2^15 for the largest and enter as
+//    two parts, 22 bits down to 2^-12 of the largest and 2^-33 of it in absolute terms.
+//    Their products with the codes are exact, sums are fp32.
 //
 // Work is split over a fixed number of workgroups by the tokens that are there: the
 // blocks of all (sequence, KV head) pairs in a row, an equal run of them for each
@@ -32,31 +35,52 @@ constexpr int kWaves = 4;
 constexpr int kPairBlocks = 16;
 constexpr float kGrow = 6.f;            // the running maximum follows once a logit is 2^6 above it
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+constexpr float kLift = 9.f;            // weights are exp2(logit - maximum + kLift)
+constexpr int kQueryTop = 14;           // binary exponent of a query row's largest element in fp16
 
-// eight codes -> eight bf16 values (exact)
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+union Half8 {                           // an MFMA operand: eight fp16 values
+  u32x4 u;
+  f16x2 p[4];
+  f16x8 v;
+};
+__device__ __forceinline__ floatx4 mfma_f16(const Half8& a, const Half8& b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0);
+}
+
+// eight codes -> eight fp16 values (exact).  int8: a byte with its sign bit turned over
+// behind 0x64 is the fp16 number 1024 + 128 + code
 template <int FMT>
-__device__ __forceinline__ Op8 codes_to_bf16(uint32_t w0, uint32_t w1) {
-  Op8 o;
+__device__ __forceinline__ Half8 codes_to_f16(uint32_t w0, uint32_t w1) {
+  Half8 o;
   if (FMT == S4R_KV_INT8) {
-    float a[4], b[4];
-    kv8_numbers<FMT>(w0, a);
-    kv8_numbers<FMT>(w1, b);
-    o.u = make_uint4(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3]));
+    w0 ^= 0x80808080u;
+    w1 ^= 0x80808080u;
+    o.u[0] = __builtin_amdgcn_perm(0x64646464u, w0, 0x04010400u);
+    o.u[1] = __builtin_amdgcn_perm(0x64646464u, w0, 0x04030402u);
+    o.u[2] = __builtin_amdgcn_perm(0x64646464u, w1, 0x04010400u);
+    o.u[3] = __builtin_amdgcn_perm(0x64646464u, w1, 0x04030402u);
+    const f16x2 zero = {(_Float16)1152.f, (_Float16)1152.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o.p[i] -= zero;
   } else {
-    o.u.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, false));
-    o.u.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, true));
-    o.u.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, false));
-    o.u.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, true));
+    o.u[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.0f, false));
+    o.u[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.0f, true));
+    o.u[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.0f, false));
+    o.u[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.0f, true));
   }
   return o;
 }
 
-// two fp32 values' upper halves as packed bf16 (truncated)
-__device__ __forceinline__ uint32_t upper2(float a, float b) {
-  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+// two fp32 values as fp16, cut off, and what is left of them
+__device__ __forceinline__ uint32_t take_f16x2(float& a, float& b) {
+  const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
+  a -= (float)h[0];
+  b -= (float)h[1];
+  return __builtin_bit_cast(uint32_t, h);
 }
-__device__ __forceinline__ float upper(float a) { return __uint_as_float(__float_as_uint(a) & 0xFFFF0000u); }
 
 // max / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48
 __device__ __forceinline__ float rows_max(float x) {
@@ -162,21 +186,28 @@ struct Order {
   }
 };
 
-// query elements as bf16 parts: bf16 as stored, fp32 in three
+// eight query elements as fp32; fp16 parts that hold them
 template <typename T>
-struct QParts;
+struct Query;
 template <>
-struct QParts<uint16_t> {
-  static constexpr int n = 1;
-  __device__ __forceinline__ static void load(const uint16_t* p, Op8* o) { o[0].u = *reinterpret_cast<const uint4*>(p); }
+struct Query<uint16_t> {
+  static constexpr int parts = 1;
+  __device__ __forceinline__ static void load(const uint16_t* p, float* x) {
+    const u32x4 u = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(u[i] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+  }
 };
 template <>
-struct QParts<float> {
-  static constexpr int n = 3;
-  __device__ __forceinline__ static void load(const float* p, Op8* o) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    split_f32x8(x, o[0], o[1], o[2]);
+struct Query<float> {
+  static constexpr int parts = 2;
+  __device__ __forceinline__ static void load(const float* p, float* x) {
+    const floatx4 a = *reinterpret_cast<const floatx4*>(p), b = *reinterpret_cast<const floatx4*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
   }
 };
 
@@ -187,25 +218,37 @@ __device__ __forceinline__ int64_t part_row(int slot, int chunks, int chunk, int
   return ((int64_t)slot * chunks + chunk) * kKv8Rows + row;
 }
 
-template <typename T, int FMT, int DH>
-__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 || DH == 64 ? 2 : 1) void k_kv8_decode(
+// RC: chunks of 16 query rows that a workgroup works on; they share its blocks and
+// their conversion
+template <typename T, int FMT, int DH, int RC>
+__global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
     const T* __restrict__ q, const uint8_t* __restrict__ k_codes, const float* __restrict__ k_scales,
     const uint8_t* __restrict__ v_codes, const float* __restrict__ v_scales, float* __restrict__ part_ml,
     float* __restrict__ part_o, float* __restrict__ out, Seqs S, int nwg, int by_pair, int chunks, int n_q, int G,
     int tiles) {
-  constexpr int NP = QParts<T>::n, NK = DH / 16, NV = DH / 16;   // 1 KiB pieces of a block per side
-  constexpr int KB = DH / 64;
-  // workgroups of one run's query chunks 8 ids apart: on one XCD, sharing its L2
-  const int id = blockIdx.x, chunk = (id >> 3) % chunks, w = (id >> 3) / chunks * 8 + (id & 7);
+  constexpr int NP = Query<T>::parts, NK = DH / 16, NV = DH / 16;   // 1 KiB pieces of a block per side
+  constexpr int KB = DH / 64, ROWS = RC * kKv8Rows;
+  // workgroups of one run's query rows 8 ids apart: on one XCD, sharing its L2
+  const int sets = (chunks + RC - 1) / RC;
+  const int id = blockIdx.x, set = (id >> 3) % sets, w = (id >> 3) / sets * 8 + (id & 7);
   if (w >= nwg) return;
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 15, kg = lane >> 4;
   const int hkv = S.hkv, hq = hkv * G, rows = n_q * G;
-  __shared__ float wm[kWaves][kKv8Rows], wl[kWaves][kKv8Rows];
-  __shared__ float wo[kWaves][kKv8Rows][DH];
+  __shared__ float wm[kWaves][ROWS], wl[kWaves][ROWS];
+  __shared__ float wo[kWaves][ROWS][DH];
 
-  const int row = chunk * kKv8Rows + col;                       // this lane's query row in the logits
-  const int back = row < rows ? n_q - 1 - row / G : 0;          // tokens that its query token does not see yet
+  // this lane's query rows in the logits, the tokens that their query tokens do not see
+  // yet, and the same of the rows it holds in the outputs
+  int row[RC], back[RC], back_out[RC][4];
+  auto not_seen = [&](int r) { return r < rows ? n_q - 1 - r / G : 0; };
+#pragma unroll
+  for (int r = 0; r < RC; ++r) {
+    row[r] = set * ROWS + r * kKv8Rows + col;
+    back[r] = not_seen(row[r]);
+#pragma unroll
+    for (int v = 0; v < 4; ++v) back_out[r][v] = not_seen(set * ROWS + r * kKv8Rows + 4 * kg + v);
+  }
   const float to_log2 = 1.4426950408889634f / sqrtf((float)DH);
 
   // a pair's blocks are [begin, end) of the line, the next pair begins at `next`;
@@ -273,24 +316,52 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 || DH == 64 ? 2 : 1) vo
     const int pa0 = after.begin + wave;                         // this wave's first block there
     const bool ahead = more && pa0 < min(after.end, u1);
     const int b = pair.b, j = pair.j, N = pair.N;
-    float M = -INFINITY, l = 0.f;
-    floatx4 acc[NV];
+    float M[RC], l[RC];
+    floatx4 acc[RC][NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < RC; ++r) {
+      M[r] = -INFINITY;
+      l[r] = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) acc[r][i] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
 
     if (p < ue) {
       if (have != p) {
         load_keys(pair.block0 + p - pair.begin);
         load_values(pair.block0 + p - pair.begin);
       }
-      Op8 qb[KB][2][NP];
-      {
-        const int r = min(row, rows - 1);
-        const T* qp = q + (((int64_t)b * n_q + r / G) * hq + (int64_t)j * G + r % G) * DH;
+      Half8 qb[RC][KB][2][NP];
+      float fq[RC];                                             // a row's power of two with 1 / sqrt(d_h) and log2 e
+#pragma unroll
+      for (int r = 0; r < RC; ++r) {
+        const int i = min(row[r], rows - 1);
+        const T* qp = q + (((int64_t)b * n_q + i / G) * hq + (int64_t)j * G + i % G) * DH;
+        float x[KB][2][8], top = 0.f;
 #pragma unroll
         for (int d = 0; d < KB; ++d)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) QParts<T>::load(qp + d * 64 + 16 * kg + 8 * h, qb[d][h]);
+          for (int h = 0; h < 2; ++h) {
+            Query<T>::load(qp + d * 64 + 16 * kg + 8 * h, x[d][h]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[d][h][e]));
+          }
+        top = rows_max(top);
+        int up;                                                 // largest element in [1/2, 1) * 2^up
+        (void)frexpf(top, &up);
+        up = top > 0.f && top < INFINITY ? up : 0;
+        fq[r] = ldexpf(to_log2, up - 1 - kQueryTop);
+#pragma unroll
+        for (int d = 0; d < KB; ++d)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[d][h][e] = ldexpf(x[d][h][e], kQueryTop + 1 - up);
+#pragma unroll
+            for (int p = 0; p < NP; ++p)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) qb[r][d][h][p].u[e] = take_f16x2(x[d][h][2 * e], x[d][h][2 * e + 1]);
+          }
       }
       do {
         const int tile = p - pair.begin;
@@ -298,75 +369,35 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 || DH == 64 ? 2 : 1) vo
         const bool on = p + kWaves < ue;
         have = on ? p + kWaves : (ahead ? pa0 : -1);
         const int block = on ? pair.block0 + tile + kWaves : (ahead ? after.block0 + wave : pair.block0 + tile);
-        // logits
-        floatx4 s[4];
+        // logits, four sums side by side: a sum's next product waits for the one before it
+        floatx4 s[RC][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-        // four sums side by side: a sum's next product waits for the one before it
+        for (int r = 0; r < RC; ++r)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[r][i] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int d = 0; d < KB; ++d)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            Op8 a[4];
+            Half8 a[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = codes_to_bf16<FMT>(kk[i * KB + d][2 * h], kk[i * KB + d][2 * h + 1]);
+            for (int i = 0; i < 4; ++i) a[i] = codes_to_f16<FMT>(kk[i * KB + d][2 * h], kk[i * KB + d][2 * h + 1]);
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
+            for (int r = 0; r < RC; ++r)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) s[i] = mfma16x16x32(a[i], qb[d][h][p], s[i]);
+              for (int p = 0; p < NP; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[r][i] = mfma_f16(a[i], qb[r][d][h][p], s[r][i]);
           }
-        const float f = sk * to_log2;
+        float f[RC];
+#pragma unroll
+        for (int r = 0; r < RC; ++r) f[r] = sk * fq[r];
         load_keys(block);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) s[i][v] *= f;
-        // tokens that a query row does not see (of the pair's last blocks only)
-        const int seen = N - back - tile * kKv8Block;           // this row sees the block's first `seen` tokens
+        // tokens that a query row does not see, or that do not exist (of a pair's last
+        // blocks only)
         const bool part = (tile + 1) * kKv8Block > N - (n_q - 1);
         if (part) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) s[i][v] = (16 * i + 4 * kg + v < seen) ? s[i][v] : -INFINITY;
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) top = fmaxf(top, s[i][v]);
-        top = rows_max(top);
-        const bool grow = top > M + kGrow;                      // also where M is -inf and a token is seen
-        if (__ballot(grow)) {
-          const float to = grow ? top : M;
-          const float a = grow ? __builtin_amdgcn_exp2f(M - to) : 1.f;
-          M = to;
-          l *= a;
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float av = __shfl(a, 4 * kg + v);             // lane r holds row r
-#pragma unroll
-            for (int i = 0; i < NV; ++i) acc[i][v] *= av;
-          }
-        }
-        const float ref = M == -INFINITY ? 0.f : M;
-        float x[4][4], sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float p = __builtin_amdgcn_exp2f(s[i][v] - ref);
-            sum += p;
-            x[i][v] = p * sv;
-          }
-        l += sum;
-        if (part) {
-          // a token that is not seen takes no part, whatever its block's scale or codes are
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int v = 0; v < 4; ++v) x[i][v] = (16 * i + 4 * kg + v < seen) ? x[i][v] : 0.f;
-          const int there = N - tile * kKv8Block;               // tokens of the block that exist
+          const int there = N - tile * kKv8Block;
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
             uint32_t m = 0;
@@ -376,41 +407,93 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 || DH == 64 ? 2 : 1) vo
             for (int i = 0; i < NV; ++i) vv[i][v] &= m;
           }
         }
-        // three parts of p * scale; contraction index 4 v + i of k-group kg
-        Op8 pa[2][3];
+        Half8 pa[RC][2][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int r = 0; r < RC; ++r) {
 #pragma unroll
-          for (int p = 0; p < 3; ++p) {
-            uint32_t o[4];
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) s[r][i][v] *= f[r];
+          const int seen = N - back[r] - tile * kKv8Block;      // this row sees the block's first `seen` tokens
+          if (part) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) s[r][i][v] = (16 * i + 4 * kg + v < seen) ? s[r][i][v] : -INFINITY;
+          }
+          float top = s[r][0][0];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) top = fmaxf(top, s[r][i][v]);
+          top = rows_max(top);
+          const bool grow = top > M[r] + kGrow;                 // also where M is -inf and a token is seen
+          if (__ballot(grow)) {
+            const float to = grow ? top : M[r];
+            const float a = grow ? __builtin_amdgcn_exp2f(M[r] - to) : 1.f;
+            M[r] = to;
+            l[r] *= a;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const float av = __shfl(a, 4 * kg + v);           // lane r holds row r
+#pragma unroll
+              for (int i = 0; i < NV; ++i) acc[r][i][v] *= av;
+            }
+          }
+          const float ref = M[r] == -INFINITY ? 0.f : M[r] - kLift;
+          float sum = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              s[r][i][v] = __builtin_amdgcn_exp2f(s[r][i][v] - ref);
+              sum += s[r][i][v];
+            }
+          l[r] += sum;
+          // two parts; contraction index 4 v + i of k-group kg
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int v = 2 * h + e / 2, i = 2 * (e % 2);
-              o[e] = upper2(x[i][v], x[i + 1][v]);
-              x[i][v] -= upper(x[i][v]);
-              x[i + 1][v] -= upper(x[i + 1][v]);
+              float x = s[r][i][v], y = s[r][i + 1][v];
+              pa[r][h][0].u[e] = take_f16x2(x, y);
+              pa[r][h][1].u[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
             }
-            pa[h][p].u = make_uint4(o[0], o[1], o[2], o[3]);
-          }
+        }
+        // the block's scale; a row that sees none of its tokens takes no part, whatever it is
+        float so[RC][4];
+#pragma unroll
+        for (int r = 0; r < RC; ++r)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) so[r][v] = part && N - back_out[r][v] <= tile * kKv8Block ? 0.f : sv;
         // a block's products from zero, then added: the matrix unit cuts what it adds to a
         // large sum, which over a run of 64 blocks had made 2.3e-6 of the result
 #pragma unroll
         for (int i0 = 0; i0 < NV; i0 += 4) {
-          floatx4 o[4];
+          floatx4 o[RC][4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) o[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+          for (int r = 0; r < RC; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[r][i] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            Op8 bv[4];
+            Half8 bv[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) bv[i] = codes_to_bf16<FMT>(vv[i0 + i][2 * h], vv[i0 + i][2 * h + 1]);
+            for (int i = 0; i < 4; ++i) bv[i] = codes_to_f16<FMT>(vv[i0 + i][2 * h], vv[i0 + i][2 * h + 1]);
 #pragma unroll
-            for (int p = 0; p < 3; ++p)
+            for (int r = 0; r < RC; ++r)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) o[i] = mfma16x16x32(pa[h][p], bv[i], o[i]);
+              for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[r][i] = mfma_f16(pa[r][h][p], bv[i], o[r][i]);
           }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[i0 + i] += o[i];
+          for (int r = 0; r < RC; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) acc[r][i0 + i][v] = fmaf(o[r][i][v], so[r][v], acc[r][i0 + i][v]);
         }
         load_values(block);
         p += kWaves;
@@ -421,20 +504,23 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 || DH == 64 ? 2 : 1) vo
       continue;
     }
     // merge the waves
-    const float ls = rows_sum(l);
-    if (kg == 0) {
-      wm[wave][col] = M;
-      wl[wave][col] = ls;
+#pragma unroll
+    for (int r = 0; r < RC; ++r) {
+      const float ls = rows_sum(l[r]);
+      if (kg == 0) {
+        wm[wave][r * kKv8Rows + col] = M[r];
+        wl[wave][r * kKv8Rows + col] = ls;
+      }
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) wo[wave][r * kKv8Rows + 4 * kg + v][16 * i + col] = acc[r][i][v];
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) wo[wave][4 * kg + v][16 * i + col] = acc[i][v];
     __syncthreads();
     const bool whole = us == pair.begin && ue == pair.end;
     const int slot = us > pair.begin ? 2 * w : 2 * w + 1;
-    for (int e = t; e < kKv8Rows * DH; e += kWaves * 64) {
-      const int r = e / DH, d = e % DH, gr = chunk * kKv8Rows + r;
+    for (int e = t; e < ROWS * DH; e += kWaves * 64) {
+      const int r = e / DH, d = e % DH, gr = set * ROWS + r;
       if (gr >= rows) break;
       float top = -INFINITY;
 #pragma unroll
@@ -450,7 +536,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 || DH == 64 ? 2 : 1) vo
       if (whole) {
         out[(((int64_t)b * n_q + gr / G) * hq + (int64_t)j * G + gr % G) * DH + d] = sum == 0.f ? 0.f : o / sum;
       } else {
-        const int64_t pr = part_row(slot, chunks, chunk, r);
+        const int64_t pr = part_row(slot, chunks, gr / kKv8Rows, gr % kKv8Rows);
         part_o[pr * DH + d] = o;
         if (d == 0) {
           part_ml[pr * 2] = top;
@@ -528,15 +614,18 @@ __global__ __launch_bounds__(256) void k_kv8_combine(const float* __restrict__ p
 }
 
 int row_chunks(const Problem& P, int n_q) { return (n_q * P.G + kKv8Rows - 1) / kKv8Rows; }
+// workgroups over the query rows: two chunks each where there are two (five query tokens
+// of four heads over 120001 tokens: 76 us in two workgroups)
+int row_sets(const Problem& P, int n_q) { return (row_chunks(P, n_q) + 1) / 2; }
 // a workgroup for each pair where the caches are short: its waves take at most
 // kPairBlocks / 4 blocks each, and nothing is left to merge
-bool one_workgroup_per_pair(const Problem& P, int chunks, int64_t n_max) {
-  return n_max <= kPairBlocks * kKv8Block && (int64_t)P.B * P.hkv * chunks <= 1 << 23;   // workgroups of a grid
+bool one_workgroup_per_pair(const Problem& P, int sets, int64_t n_max) {
+  return n_max <= kPairBlocks * kKv8Block && (int64_t)P.B * P.hkv * sets <= 1 << 23;   // workgroups of a grid
 }
 // runs of a call over at most n_max tokens per sequence: a block for every wave at least
 int runs(const Problem& P, int n_q, int64_t n_max) {
   const int64_t blocks = (int64_t)P.B * P.hkv * pair_length((int)((n_max + kKv8Block - 1) / kKv8Block), 1 << 30);
-  return (int)std::max<int64_t>(1, std::min<int64_t>((blocks + kWaves - 1) / kWaves, kKv8Wgs / row_chunks(P, n_q)));
+  return (int)std::max<int64_t>(1, std::min<int64_t>((blocks + kWaves - 1) / kWaves, kKv8Wgs / row_sets(P, n_q)));
 }
 
 }  // namespace
@@ -549,18 +638,25 @@ size_t kv8_ws_bytes(const Problem& P, int n_q) {
 
 hipError_t launch_kv8_decode(const Problem& P, const Kv8& C, int64_t n_max, const int32_t* lengths, int n_q,
                              const void* q, float* out, void* ws, hipStream_t st) {
-  const int chunks = row_chunks(P, n_q);
-  const bool by_pair = one_workgroup_per_pair(P, chunks, n_max);
+  const int chunks = row_chunks(P, n_q), sets = row_sets(P, n_q);
+  const bool by_pair = one_workgroup_per_pair(P, sets, n_max);
   const int nwg = by_pair ? P.B * P.hkv : runs(P, n_q, n_max);
   const size_t part_rows = (size_t)2 * nwg * chunks * kKv8Rows;
   float* part_o = (float*)ws;
   float* part_ml = part_o + part_rows * P.dh;
   const Seqs S{lengths, (int)n_max, P.B, P.hkv};
-  const dim3 grid((nwg + 7) / 8 * 8 * chunks);
+  const dim3 grid((nwg + 7) / 8 * 8 * sets);
   auto go = [&](auto elem, auto fmt, auto dh) {
     using T = decltype(elem);
-    hipLaunchKernelGGL((k_kv8_decode<T, fmt(), dh()>), grid, dim3(kWaves * 64), 0, st, (const T*)q, C.k_codes, C.k_scales,
-                       C.v_codes, C.v_scales, part_ml, part_o, out, S, nwg, (int)by_pair, chunks, n_q, P.G, kv8_tiles(P));
+    auto with = [&](auto rc) {
+      hipLaunchKernelGGL((k_kv8_decode<T, fmt(), dh(), rc()>), grid, dim3(kWaves * 64), 0, st, (const T*)q, C.k_codes,
+                         C.k_scales, C.v_codes, C.v_scales, part_ml, part_o, out, S, nwg, (int)by_pair, chunks, n_q,
+                         P.G, kv8_tiles(P));
+    };
+    if (chunks == 1)
+      with(std::integral_constant<int, 1>());
+    else
+      with(std::integral_constant<int, 2>());
   };
   auto by_fmt = [&](auto elem, auto dh) {
     if (C.format == S4R_KV_INT8)

@@ -137,8 +137,8 @@ def attention(cache, q, lengths):
     measured below 4.6, and one rounding for each of the at most 12 that follow each other), two roundings of the
     factor, one of the difference to the maximum: at most 25 * 2^-24 S.  It changes a weight by that relative
     amount, and the sum by no more: 50 S.  exp2 is within 2^-22, twice: 8.  A lane adds 16 weights a block and a
-    matrix instruction chain six roundings a block, over at most t blocks of one wave; three-part weights, scale and
-    merges: 32 together.  All relative to sum p |v| / sum p <= max |v|."""
+    matrix instruction chain six roundings a block, over at most t blocks of one wave; weights of 22 bits, scale
+    and merges: 32 together.  All relative to sum p |v| / sum p <= max |v|."""
     B, n, hq, dh = q.shape
     G = hq // cache.H
     out, tol = np.zeros((B, n, hq, dh)), np.zeros((B, n, hq))
