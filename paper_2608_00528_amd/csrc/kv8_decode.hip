@@ -32,7 +32,6 @@ namespace s4r {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kPairBlocks = 16;
 constexpr float kGrow = 6.f;            // the running maximum follows once a logit is 2^6 above it
 
 constexpr float kLift = 9.f;            // weights are exp2(logit - maximum + kLift)
@@ -617,10 +616,15 @@ int row_chunks(const Problem& P, int n_q) { return (n_q * P.G + kKv8Rows - 1) / 
 // workgroups over the query rows: two chunks each where there are two (five query tokens
 // of four heads over 120001 tokens: 76 us in two workgroups)
 int row_sets(const Problem& P, int n_q) { return (row_chunks(P, n_q) + 1) / 2; }
-// a workgroup for each pair where the caches are short: its waves take at most
-// kPairBlocks / 4 blocks each, and nothing is left to merge
+// a workgroup for each pair where the caches are short: its waves take 4 blocks each at
+// most, 8 where the pairs fill half the chip, and nothing is left to merge.  One launch
+// against two, in a graph: 1024 tokens, 8 pairs 9.6 / 9.2 us (calls from Python 10.0 /
+// 11.8), 128 pairs 10.8 / 13.0; 2048 tokens, 8 pairs 15.4 / 10.0, 128 pairs 16.1 / 17.6,
+// 512 pairs 46.0 / 47.0
 bool one_workgroup_per_pair(const Problem& P, int sets, int64_t n_max) {
-  return n_max <= kPairBlocks * kKv8Block && (int64_t)P.B * P.hkv * sets <= 1 << 23;   // workgroups of a grid
+  const int64_t groups = (int64_t)P.B * P.hkv * sets;
+  const int blocks = groups >= 128 ? 8 * kWaves : 4 * kWaves;
+  return n_max <= (int64_t)blocks * kKv8Block && groups <= 1 << 23;   // workgroups of a grid
 }
 // runs of a call over at most n_max tokens per sequence: a block for every wave at least
 int runs(const Problem& P, int n_q, int64_t n_max) {
