@@ -113,13 +113,14 @@ __device__ __forceinline__ void kv8_numbers(uint32_t w, float (&x)[4]) {
   }
 }
 
-// rows a call writes to or reads from sequence b: [start, start + count), none
-// where they do not lie inside the cache
+// rows a call writes to or reads from sequence b: [start, start + count), none (and
+// start 0, so no block lies before the first row) where there are none or they do not
+// lie inside the cache
 __device__ __forceinline__ void kv8_rows(const int32_t* starts, const int32_t* counts, int b, int64_t row0, int n_rows,
                                          int64_t cap, int64_t& start, int& count) {
   start = starts ? (int64_t)starts[b] : row0;
   count = counts ? min(max(counts[b], 0), n_rows) : n_rows;
-  if (start < 0 || start + count > cap) start = 0, count = 0;
+  if (count == 0 || start < 0 || start + count > cap) start = 0, count = 0;
 }
 
 }  // namespace s4r

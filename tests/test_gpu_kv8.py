@@ -110,6 +110,24 @@ def test_one_start_for_all_and_strided_rows(fmt):
     assert np.array_equal(k.double().cpu().numpy(), want["k"]) and np.array_equal(v.double().cpu().numpy(), want["v"])
 
 
+@pytest.mark.parametrize("row0", [0, 5, 70, 208])
+def test_counts_of_zero_write_nothing(row0):
+    """A sequence without new rows, wherever it would have begun inside a block, stays as it is and reads as zeros."""
+    B, H, dh, cap, n = 3, 2, 64, 208, 9
+    rng = np.random.default_rng(row0)
+    ref = R.RefCache("int8", B, H, dh, cap, rng)
+    c = cfg(B, H, H, dh, cap)
+    cache = to_gpu(ref)
+    x = rows(rng, B, n, H, dh, "bf16")
+    k, v = dev(x["k"], c), dev(x["v"], c)
+    s4r.kv8_write(c, cache, k, v, row0=row0, counts=ints([0, -3, 0]))
+    s4r.kv8_write(c, cache, k, v, starts=ints([row0, 207, -1]), counts=ints([0, 0, 4]))
+    same(cache, ref)
+    for kw in (dict(row0=row0, counts=ints([0, 0, -1])), dict(starts=ints([row0, 208, 300]), counts=ints([0, 0, 5]))):
+        a, b = s4r.kv8_read(c, cache, n, **kw)
+        assert not a.any() and not b.any()
+
+
 @pytest.mark.parametrize("fmt", ["int8", "e4m3"])
 def test_appending_one_by_one_follows_the_rule(fmt):
     """Seventy tokens of growing size, one call each: the scale of a block grows again and again."""
