@@ -247,6 +247,100 @@ def test_several_query_tokens(hq, hkv, nq):
         assert torch.all(got[b, :max(nq - n, 0)] == 0)
 
 
+@pytest.mark.parametrize("fmt,dtype", [("int8", "bf16"), ("e4m3", "fp32")])
+@pytest.mark.parametrize("hq,hkv,dh", SHAPES)
+def test_attention_cut_into_runs(fmt, dtype, hq, hkv, dh):
+    """A large bound: the work is split by the tokens that are there, pairs of one block and of many are cut and
+    merged."""
+    lengths = [0, 1, 63, 2999, 64, 65, 0, 700, 1009, 257, 0]
+    B, cap = len(lengths), 3008
+    rng = np.random.default_rng(hq + dh)
+    ref = filled(rng, fmt, B, hkv, dh, cap, lengths, dtype)
+    c = cfg(B, hq, hkv, dh, cap, dtype)
+    q = R.round_to(rng.standard_normal((B, 1, hq, dh)) * 1.5, dtype)
+    _, got = check_attention(ref, c, q, lengths, cap)
+    assert torch.all(got[[0, 6, 10]] == 0)
+
+
+@pytest.mark.parametrize("fmt,dtype,hq,hkv,dh,nq", [
+    ("int8", "bf16", 8, 2, 128, 3), ("e4m3", "fp32", 28, 4, 128, 5), ("int8", "fp32", 4, 4, 64, 128),
+    ("e4m3", "bf16", 16, 1, 64, 8), ("int8", "bf16", 32, 8, 128, 12), ("e4m3", "bf16", 8, 2, 128, 5)])
+def test_several_query_tokens_cut_into_runs(fmt, dtype, hq, hkv, dh, nq):
+    lengths = [nq - 1, 0, 2200, nq, 1, 200, 513]
+    B, cap = len(lengths), 2208
+    rng = np.random.default_rng(nq + hq)
+    ref = filled(rng, fmt, B, hkv, dh, cap, lengths, dtype)
+    c = cfg(B, hq, hkv, dh, cap, dtype)
+    q = R.round_to(rng.standard_normal((B, nq, hq, dh)), dtype)
+    _, got = check_attention(ref, c, q, lengths, cap)
+    for b, n in enumerate(lengths):
+        assert torch.all(got[b, :max(nq - n, 0)] == 0)
+
+
+@pytest.mark.parametrize("n_max", [2100, 130])
+@pytest.mark.parametrize("given", [True, False])
+def test_more_sequences_than_lanes(n_max, given):
+    """Every sequence holds the same tokens up to its own length; each is compared with the one-sequence reference."""
+    B, hq, hkv, dh = 150, 4, 2, 64
+    rng = np.random.default_rng(n_max)
+    one = filled(rng, "int8", 1, hkv, dh, 2112, [n_max])
+    c = cfg(B, hq, hkv, dh, 2112)
+    t = {}
+    for s in "kv":
+        t[s + "_codes"] = torch.from_numpy(one.codes[s]).cuda().repeat(B, 1, 1, 1)
+        t[s + "_scales"] = torch.from_numpy(one.scales[s]).cuda().repeat(B, 1, 1)
+    cache = s4r.KV8Cache("int8", **t)
+    lengths = [n_max] * B
+    if given:
+        lengths = [int(x) for x in rng.integers(0, 200, B)]
+        for b in (0, 63, 64, 127, 128, 149):
+            lengths[b] = n_max
+        lengths[65:70] = [0] * 5
+        lengths = [min(x, n_max) for x in lengths]
+    q = R.round_to(rng.standard_normal((1, 1, hq, dh)), "bf16")
+    got = s4r.kv8_decode(c, cache, n_max, dev(np.tile(q, (B, 1, 1, 1)), c), s4r.alloc_kv8_workspace(c),
+                         lengths=ints(lengths) if given else None).double().cpu().numpy()
+    for n in sorted(set(lengths)):
+        want, tol = R.attention(one, q, [n])
+        at = [b for b in range(B) if lengths[b] == n]
+        assert np.all(np.abs(got[at] - want).max(-1) <= tol), n
+
+
+def test_no_tokens_anywhere():
+    B, hq, hkv, dh, cap = 70, 8, 2, 128, 4096
+    c = cfg(B, hq, hkv, dh, cap)
+    cache = s4r.kv8_alloc(c, "e4m3")
+    q = torch.ones(B, 1, hq, dh, dtype=torch.bfloat16, device="cuda")
+    ws = s4r.alloc_kv8_workspace(c)
+    for bound in (4096, 100):
+        out = torch.full((B, 1, hq, dh), 5.0, device="cuda")
+        s4r.kv8_decode(c, cache, bound, q, ws, lengths=ints([0] * B), out=out)
+        assert not out.any()
+
+
+def test_two_streams_with_their_own_workspaces():
+    """Two calls at once over one cache."""
+    B, hq, hkv, dh, cap = 2, 8, 2, 128, 8192
+    rng = np.random.default_rng(31)
+    c = cfg(B, hq, hkv, dh, cap)
+    ref = filled(rng, "int8", B, hkv, dh, cap, [5000, 2300])
+    cache, lengths = to_gpu(ref), ints([5000, 2300])
+    qs = [R.round_to(rng.standard_normal((B, 1, hq, dh)), "bf16") for _ in range(2)]
+    gq = [dev(q, c) for q in qs]
+    streams, ws = [torch.cuda.Stream() for _ in qs], [s4r.alloc_kv8_workspace(c) for _ in qs]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(10):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(s4r.kv8_decode(c, cache, cap, gq[i], ws[i], lengths=lengths))
+    torch.cuda.synchronize()
+    for i in range(2):
+        want, tol = R.attention(ref, qs[i], [5000, 2300])
+        assert np.all(np.abs(outs[i][0].double().cpu().numpy() - want).max(-1) <= tol)
+        assert all(torch.equal(o, outs[i][0]) for o in outs[i])
+
+
 def test_many_sequences_and_lengths_past_the_bound():
     """More sequences than lanes of a wave; lengths above n_tokens and below zero are clamped."""
     B, hq, hkv, dh, cap = 150, 4, 1, 64, 272
@@ -278,25 +372,31 @@ def test_logits_far_apart_and_growing():
     check_attention(ref, cfg(B, hq, hkv, dh, 3008), q, [n], n)
 
 
-def test_not_finite_blocks_reach_only_who_sees_them():
-    B, hq, hkv, dh, cap, nq = 2, 4, 2, 64, 256, 2
+@pytest.mark.parametrize("cap", [256, 2304])
+def test_not_finite_blocks_reach_only_who_sees_them(cap):
+    B, hq, hkv, dh, nq = 2, 4, 2, 64, 2
     rng = np.random.default_rng(4)
     ref = filled(rng, "e4m3", B, hkv, dh, cap, [193, 193])
     ref.scales["v"][0, 1, 1] = np.nan                  # a block in the middle, of one KV head
     ref.scales["k"][1, 0, 3] = np.nan                  # the block of the last token alone
+    ref.scales["v"][1, 1, 3] = np.inf                  # the same for its values
     c = cfg(B, hq, hkv, dh, cap)
     q = R.round_to(rng.standard_normal((B, nq, hq, dh)), "bf16")
-    got = s4r.kv8_decode(c, to_gpu(ref), 193, dev(q, c), s4r.alloc_kv8_workspace(c, nq)).cpu().numpy()
+    got = s4r.kv8_decode(c, to_gpu(ref), cap, dev(q, c), s4r.alloc_kv8_workspace(c, nq), lengths=ints([193, 193]))
+    got = got.cpu().numpy()
     bad = np.isnan(got).all(-1)
     want = np.zeros((B, nq, hq), bool)
     want[0, :, 2:] = True
     want[1, 1, :2] = True                              # its first query token does not see token 192
-    assert np.array_equal(bad, want) and np.isfinite(got[~want]).all()
+    assert np.array_equal(bad, want)
+    want[1, 1, 2:] = True
+    assert np.isfinite(got[~want]).all() and not np.isfinite(got[1, 1, 2:]).all(-1).any()
 
 
-def test_what_lies_behind_a_sequence_is_not_read():
+@pytest.mark.parametrize("cap", [512, 2304])
+def test_what_lies_behind_a_sequence_is_not_read(cap):
     """Other tokens behind the length, NaN codes among them, change nothing; outputs of a repeat are the same bits."""
-    B, hq, hkv, dh, cap = 2, 8, 2, 128, 512
+    B, hq, hkv, dh = 2, 8, 2, 128
     lengths = [70, 333]
     rng = np.random.default_rng(6)
     ref = filled(rng, "e4m3", B, hkv, dh, cap, lengths)

@@ -83,6 +83,29 @@ def test_one_side_without_weights(dtype):
     assert none is None and torch.equal(k2, k)
 
 
+def test_more_tokens_than_a_grid_holds():
+    """Rows past 2^32 elements and more tokens than one wave each: the first, the last and some between."""
+    hq, hkv, dh, n, width = 2, 2, 64, (1 << 22) + 77, 1024
+    c = cfg(hq, hkv, dh, 1e4)
+    assert n * width > 2 ** 32
+    f = torch.zeros(n, width, dtype=torch.bfloat16, device="cuda")
+    rng = np.random.default_rng(5)
+    at = np.array([0, 1, 12345, 1 << 21, (1 << 22) - 1, 1 << 22, n - 2, n - 1])
+    x = R.round_to(rng.standard_normal((len(at), hq + hkv, dh)), "bf16")
+    f[torch.from_numpy(at).cuda(), :(hq + hkv) * dh] = dev(x, c).flatten(1)
+    heads = f[:, :(hq + hkv) * dh].view(n, hq + hkv, dh)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    w = torch.ones(dh, dtype=torch.bfloat16, device="cuda")
+    q, k = s4r.qk_norm_rope(c, heads[:, :hq], heads[:, hq:], pos, w, w, k_out=heads[:, hq:])
+    index = torch.from_numpy(at).cuda()
+    # the angle's error grows with the position: 2^-53 of the frequency times 2^22
+    check(q[index], x[:, :hq], np.ones(dh), 1e-6, at, 1e4, "bf16")
+    check(k[index], x[:, hq:], np.ones(dh), 1e-6, at, 1e4, "bf16")
+    q[index] = 0
+    heads[index] = 0
+    assert not q.any() and not f.any()
+
+
 def test_far_and_negative_positions():
     c = cfg(4, 4, 128, 5e5, "fp32")
     pos = np.array([0, 1, -1, -131072, 2 ** 20 + 1, 2 ** 24 + 3, 5, 131071])
@@ -150,13 +173,13 @@ def layer(rng, B, n, hq, hkv, dh):
     return R.round_to(rng.standard_normal((B, n, hq + 2 * hkv, dh)) * 2, "bf16")
 
 
-@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
-def test_prompt_then_decoding_eager_and_replayed(fmt):
+@pytest.mark.parametrize("fmt,cap", [("int8", 272), ("e4m3", 272), ("int8", 4096), ("e4m3", 4096)])
+def test_prompt_then_decoding_eager_and_replayed(fmt, cap):
     """A decoding program: prompts of unequal lengths go in, then every step norms and rotates its heads, appends its
     token and attends.  Two steps' graphs share a workspace and are replayed in turn while lengths live on the
     device; eager steps run between the replays.  Every step is compared with the 64-bit attention over the
     reference's cache, whose keys are the kernel's own rotated rows (compared with the reference apart)."""
-    B, hq, hkv, dh, cap = 3, 8, 2, 128, 272
+    B, hq, hkv, dh = 3, 8, 2, 128
     rng = np.random.default_rng(11)
     c = cfg(hq, hkv, dh, THETA, batch=B, capacity=cap)
     wq, wk = (R.round_to(1 + 0.2 * rng.standard_normal(dh), "bf16") for _ in range(2))
