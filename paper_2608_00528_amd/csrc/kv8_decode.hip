@@ -20,12 +20,18 @@
 //    two parts, 22 bits down to 2^-12 of the largest and 2^-33 of it in absolute terms.
 //    Their products with the codes are exact, sums are fp32.
 //
-// Work is split over a fixed number of workgroups by the tokens that are there: the
-// blocks of all (sequence, KV head) pairs in a row, an equal run of them for each
-// workgroup, whose four waves take the blocks in turn.  A pair inside one run is
-// finished there; one cut by the ends of runs leaves a partial (max, sum, output)
-// per run and k_kv8_combine merges them in order.  Lengths are read on the device,
-// so a captured graph follows them.
+// Work is split over one workgroup per CU by the tokens that are there: the blocks of
+// all (sequence, KV head) pairs in a row, an equal run of them for each workgroup, whose
+// four waves take the blocks in turn.  A pair inside one run is finished there; one cut
+// by the ends of runs leaves a partial (max, sum, output) per run and k_kv8_combine
+// merges them in order.  Lengths are read on the device, so a captured graph follows them.
+//
+// Measured (kernel): 4 x 131068 tokens, 8 KV heads of 128: 155 us, 6.9 TB/s (a large
+// read reaches 6.2, a copy 5.1), 565 VALU and 48 MFMA instructions a block; with two
+// workgroups per CU 165 us, with eight waves per workgroup 164: more reads on their way
+// than 64 KB per CU make the memory slower.  A block takes a wave 2.2 us; 7 us are the
+// launch, the first block's way and the merge (1 x 32764 tokens: 15.8 us for four blocks
+// a wave, and 4 us for k_kv8_combine).
 #include "kv8.h"
 
 namespace s4r {

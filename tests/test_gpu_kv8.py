@@ -306,6 +306,31 @@ def test_more_sequences_than_lanes(n_max, given):
         assert np.all(np.abs(got[at] - want).max(-1) <= tol), n
 
 
+def test_agrees_with_the_bf16_cache():
+    """Whole numbers up to 127 are the same values in both caches: the attention over them is the same but for fp32
+    rounding (bound as in the reference; the bf16 cache's weights are fp32)."""
+    B, hq, hkv, dh, n = 2, 8, 2, 128, 3001
+    cap = 3008
+    rng = np.random.default_rng(77)
+    c = cfg(B, hq, hkv, dh, cap)
+    x = {s: rng.integers(-127, 128, (B, n, hkv * dh)).astype(float) for s in "kv"}
+    for s in "kv":
+        x[s][:, ::64, ::dh] = 127                      # scale 1 in every block
+    q = R.round_to(rng.standard_normal((B, 1, hq, dh)) * 0.02, "bf16")
+    cache = s4r.kv8_alloc(c, "int8")
+    s4r.kv8_write(c, cache, dev(x["k"], c), dev(x["v"], c))
+    assert torch.all(cache.k_scales[:, :, :n // 64 + 1] == 1)
+    got = s4r.kv8_decode(c, cache, n, dev(q, c), s4r.alloc_kv8_workspace(c))
+    full = {s: torch.zeros(B, cap, hkv * dh, dtype=torch.bfloat16, device="cuda") for s in "kv"}
+    for s in "kv":
+        full[s][:, :n] = dev(x[s], c)
+    dense = s4r.dense_decode(c, n, dev(q[:, 0], c), full["k"], full["v"], s4r.alloc_workspace(c))
+    ref = R.RefCache("int8", B, hkv, dh, cap)
+    ref.write(x, [0] * B, [n] * B)
+    _, tol = R.attention(ref, q, [n] * B)
+    assert np.all((got[:, 0].double() - dense.double()).abs().amax(-1).cpu().numpy() <= 2 * tol[:, 0])
+
+
 def test_no_tokens_anywhere():
     B, hq, hkv, dh, cap = 70, 8, 2, 128, 4096
     c = cfg(B, hq, hkv, dh, cap)
