@@ -412,8 +412,9 @@ s4r_status s4r_dense_decode(const s4r_config* cfg, int64_t N, const void* q, con
  *   q_weight, k_weight [d_h] storage dtype or NULL; eps finite and >= 0.
  *   positions int32 [n_tokens], 4-byte aligned, any values (NULL only when
  *   rope_theta is 0).
- * Sums of squares are fp64, everything else fp32, rounded once.  Uses cfg's head
- * counts, head_dim, rope_theta and dtype.
+ * Sums of squares are fp32, and fp64 for heads whose squares leave its range; the
+ * angle is exact to 2^-25 of a revolution; rounded once.  Uses cfg's head counts,
+ * head_dim, rope_theta and dtype.
  */
 s4r_status s4r_qk_norm_rope(const s4r_config* cfg, int64_t n_tokens, const void* q, int64_t q_stride,
                             const void* k, int64_t k_stride, const void* q_weight, const void* k_weight,

@@ -579,16 +579,16 @@ def _kv8(cfg, cache, dev):
         raise ValueError("cache must be a KV8Cache")
     blocks = cfg.batch * cfg.n_kv_heads * ((cfg.capacity + L.KV8_BLOCK - 1) // L.KV8_BLOCK)
     codes = blocks * L.KV8_BLOCK * cfg.head_dim
-    view = [_KV_FORMATS[cache.format]]
-    for name, t, dt, n in (("k_codes", cache.k_codes, torch.uint8, codes),
-                           ("k_scales", cache.k_scales, torch.float32, blocks),
-                           ("v_codes", cache.v_codes, torch.uint8, codes),
-                           ("v_scales", cache.v_scales, torch.float32, blocks)):
-        view.append(_ptr(t, name, dt))
+    kc, ks, vc, vs = cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales
+    view = L.KV8(_KV_FORMATS[cache.format], _ptr(kc, "k_codes", torch.uint8), _ptr(ks, "k_scales", torch.float32),
+                 _ptr(vc, "v_codes", torch.uint8), _ptr(vs, "v_scales", torch.float32))
+    for name, t, n in (("k_codes", kc, codes), ("k_scales", ks, blocks), ("v_codes", vc, codes),
+                       ("v_scales", vs, blocks)):
         if t.numel() != n:
             raise ValueError(f"{name} has {t.numel()} elements, expected {n}")
-        _here(t, name, dev)
-    return ctypes.byref(L.KV8(*view))
+        if t.get_device() != dev:
+            _here(t, name, dev)
+    return ctypes.byref(view)
 
 
 def kv8_write(cfg, cache, k, v, row0=0, starts=None, counts=None):
