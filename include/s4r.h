@@ -461,7 +461,9 @@ s4r_status s4r_kv8_size(const s4r_config* cfg, size_t* code_bytes, size_t* scale
  * A sequence whose range does not lie in [0, capacity) is left as it is.
  *   A call that starts inside a block keeps the block's earlier tokens: the scale
  * becomes the larger of the present one and the new rows' own, and where it grows
- * the earlier tokens are written anew from the values they stood for.  A call
+ * the earlier tokens are written anew from the values they stood for (rounded once
+ * more: at most half a step of the new scale; a power of two changes only e4m3 numbers
+ * that become subnormal).  A call
  * that starts at a block's first token sets the scale afresh.  The earlier tokens
  * must have been written, or the cache have been zeros.  Tokens of a block
  * behind the last one written keep their codes (their scale may have changed: a

@@ -46,7 +46,7 @@ def check(got, x, weight, eps, pos, theta, dtype):
 @pytest.mark.parametrize("hq,hkv,dh,theta", [(32, 8, 128, 1e6), (8, 2, 64, 1e4), (28, 4, 128, 5e5), (4, 4, 128, 1e4),
                                              (5, 1, 64, 1e4), (16, 1, 128, 0.0), (3, 3, 64, 0.0)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("tokens", [1, 7, 301])
+@pytest.mark.parametrize("tokens", [1, 7, 301, 900])
 def test_heads_in_rows_of_a_fused_projection(hq, hkv, dh, theta, dtype, tokens):
     rng = np.random.default_rng(tokens + hq)
     c = cfg(hq, hkv, dh, theta, dtype)
