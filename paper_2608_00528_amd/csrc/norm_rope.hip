@@ -191,8 +191,9 @@ hipError_t launch_qk_norm_rope(const Problem& P, int64_t n_tokens, const void* q
   // few tokens: a wave for each group of heads; many: a token's heads in one wave,
   // which then works out the token's turns once (32764 tokens of 32 + 8 heads: 131 us,
   // 5.1 TB/s; waves that take several tokens, 256 to 1536 workgroups in all: 133 to
-  // 160 us; stores through the caches 135 us)
-  const int per = n_tokens * groups <= 4096 ? 1 : groups;
+  // 160 us; stores through the caches 135 us).  One side / the other: 32 tokens 3.8 / 8.1
+  // us, 512 tokens 6.1 / 8.8, 1000 tokens 10.0 / 9.7, 2000 tokens 16.4 / 11.1
+  const int per = n_tokens * groups <= 8192 ? 1 : groups;
   const int64_t units = n_tokens * ((groups + per - 1) / per);
   const dim3 grid((unsigned)std::min<int64_t>((units + 3) / 4, 1 << 20));
   auto go = [&](auto elem, auto dh) {
