@@ -413,8 +413,8 @@ s4r_status s4r_dense_decode(const s4r_config* cfg, int64_t N, const void* q, con
  *   positions int32 [n_tokens], 4-byte aligned, any values (NULL only when
  *   rope_theta is 0).
  * Sums of squares are fp32, and fp64 for heads whose squares leave its range; the
- * angle is exact to 2^-25 of a revolution; rounded once.  Uses cfg's head counts,
- * head_dim, rope_theta and dtype.
+ * angle is exact to 2^-25 of a revolution for positions below 2^26, to 2^-21 for
+ * any; rounded once.  Uses cfg's head counts, head_dim, rope_theta and dtype.
  */
 s4r_status s4r_qk_norm_rope(const s4r_config* cfg, int64_t n_tokens, const void* q, int64_t q_stride,
                             const void* k, int64_t k_stride, const void* q_weight, const void* k_weight,
@@ -495,7 +495,8 @@ s4r_status s4r_kv8_read(const s4r_config* cfg, const s4r_kv8* cache, int64_t n_r
  * the work follows the lengths on the device, so a captured graph may be replayed
  * as sequences grow up to N.  A query token that sees nothing gets zeros.  Query
  * elements must be finite.  1 <= N <= capacity, 1 <= n_q and n_q * G <= 128.
- * ws: s4r_kv8_workspace_size bytes, 256-byte aligned; its contents do not matter.
+ * ws: s4r_kv8_workspace_size bytes, 256-byte aligned (that of a larger n_q serves
+ * too); its contents do not matter.
  * Sums are fp32.  The codes enter the matrix cores exactly, and so do the elements of
  * a bf16 query row down to 2^-28 of its largest; fp32 queries and the softmax weights
  * enter with 22 bits.

@@ -653,9 +653,12 @@ int runs(const Problem& P, int n_q, int64_t n_max) {
 
 }  // namespace
 
-// (max, sum) and d_h sums for two slots per run, sixteen rows per chunk
+// (max, sum) and d_h sums for two slots per run, sixteen rows per chunk; what a call
+// with fewer query tokens needs is inside
 size_t kv8_ws_bytes(const Problem& P, int n_q) {
-  const size_t part_rows = (size_t)2 * runs(P, n_q, P.cap) * row_chunks(P, n_q) * kKv8Rows;
+  size_t part_rows = 0;
+  for (int n = 1; n <= n_q; ++n)
+    part_rows = std::max(part_rows, (size_t)2 * runs(P, n, P.cap) * row_chunks(P, n) * kKv8Rows);
   return part_rows * (P.dh + 2) * sizeof(float);
 }
 

@@ -41,6 +41,11 @@ def test_sizes():
     assert s4r.kv8_size(cfg(head_dim=128, batch=1, capacity=64)) == (2 * 64 * 128, 2)
     one, two = s4r.kv8_workspace_size(cfg()), s4r.kv8_workspace_size(cfg(), 32)
     assert 0 < one < two and one % 256 == 0 and two % 256 == 0
+    # a workspace serves every smaller number of query tokens
+    for c in (cfg(), cfg(capacity=131072), cfg(n_q_heads=16, n_kv_heads=1, head_dim=128), cfg(n_q_heads=4, n_kv_heads=4, capacity=16)):
+        g = c.n_q_heads // c.n_kv_heads
+        sizes = [s4r.kv8_workspace_size(c, n) for n in range(1, 128 // g + 1)]
+        assert sizes == sorted(sizes)
     for n in (0, 33):                                   # n * G = 132 > 128
         with pytest.raises(s4r.S4RError):
             s4r.kv8_workspace_size(cfg(), n)
