@@ -25,6 +25,7 @@
 // four waves take the blocks in turn.  A pair inside one run is finished there; one cut
 // by the ends of runs leaves a partial (max, sum, output) per run and k_kv8_combine
 // merges them in order.  Lengths are read on the device, so a captured graph follows them.
+// Short caches have a workgroup or, in large batches, a wave for each pair instead.
 //
 // Measured (kernel): 4 x 131068 tokens, 8 KV heads of 128: 155 us, 6.9 TB/s (a large
 // read reaches 6.2, a copy 5.1), 565 VALU and 48 MFMA instructions a block; with two
@@ -224,8 +225,10 @@ __device__ __forceinline__ int64_t part_row(int slot, int chunks, int chunk, int
 }
 
 // RC: chunks of 16 query rows that a workgroup works on; they share its blocks and
-// their conversion
-template <typename T, int FMT, int DH, int RC>
+// their conversion.  SHARE: waves that take a pair's blocks in turn - the workgroup's, or
+// 1: a pair to each wave, nothing to merge, and a workgroup's waves never wait for each
+// other (one_wave_per_pair)
+template <typename T, int FMT, int DH, int RC, int SHARE>
 __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
     const T* __restrict__ q, const uint8_t* __restrict__ k_codes, const float* __restrict__ k_scales,
     const uint8_t* __restrict__ v_codes, const float* __restrict__ v_scales, float* __restrict__ part_ml,
@@ -233,15 +236,18 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
     int tiles) {
   constexpr int NP = Query<T>::parts, NK = DH / 16, NV = DH / 16;   // 1 KiB pieces of a block per side
   constexpr int KB = DH / 64, ROWS = RC * kKv8Rows;
+  static_assert(SHARE == 1 || SHARE == kWaves, "a wave or a workgroup per pair");
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   // workgroups of one run's query rows 8 ids apart: on one XCD, sharing its L2
   const int sets = (chunks + RC - 1) / RC;
-  const int id = blockIdx.x, set = (id >> 3) % sets, w = (id >> 3) / sets * 8 + (id & 7);
+  const int id = blockIdx.x, set = (id >> 3) % sets, wg = (id >> 3) / sets * 8 + (id & 7);
+  const int w = SHARE == 1 ? wg * kWaves + wave : wg, turn = SHARE == 1 ? 0 : wave;
   if (w >= nwg) return;
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int col = lane & 15, kg = lane >> 4;
   const int hkv = S.hkv, hq = hkv * G, rows = n_q * G;
-  __shared__ float wm[kWaves][ROWS], wl[kWaves][ROWS];
-  __shared__ float wo[kWaves][ROWS][DH];
+  constexpr int MROWS = SHARE == 1 ? 1 : ROWS;                  // rows to merge
+  __shared__ float wm[SHARE][MROWS], wl[SHARE][MROWS];
+  __shared__ float wo[SHARE][MROWS][DH];
 
   // this lane's query rows in the logits, the tokens that their query tokens do not see
   // yet, and the same of the rows it holds in the outputs
@@ -276,7 +282,7 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
   };
   Pair pair, after;
   int u0 = 0, u1;                                               // this workgroup's run
-  if (by_pair) {
+  if (SHARE == 1 || by_pair) {
     pair.b = w / hkv;
     pair.j = w - pair.b * hkv;
     pair.N = __builtin_amdgcn_readfirstlane(S.tokens(pair.b));
@@ -310,26 +316,26 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
   // meet on the same memory channels (8 x 16256 tokens, 8 KV heads: 55 us; so 48 us).
   // The block of a pair that is read for position p of its part [us, ue):
   auto block_at = [&](const Pair& at, int p, int us, int ue) __attribute__((always_inline)) {
-    const int rounds = (ue - us) / kWaves, turned = us + rounds * kWaves;
-    int x = p + ((w & 15) * rounds >> 4) * kWaves;
-    x -= x >= turned ? rounds * kWaves : 0;
+    const int rounds = (ue - us) / SHARE, turned = us + rounds * SHARE;
+    int x = p + ((w & 15) * rounds >> 4) * SHARE;
+    x -= x >= turned ? rounds * SHARE : 0;
     return (p < turned ? x : p) - at.begin;
   };
   // a wave takes every fourth block of the run, its next one on the way while it works
   // on one, also where that lies in the next pair
-  int p = u0 + wave, have = -1;
+  int p = u0 + turn, have = -1;
   if (p < min(pair.end, u1)) {
     have = p;
     const int block = pair.block0 + block_at(pair, p, u0, min(pair.end, u1));
     load_keys(block);
     load_values(block);
   }
-  for (int us = u0;; us = after.begin, p = us + wave, pair = after) {
+  for (int us = u0;; us = after.begin, p = us + turn, pair = after) {
     const int ue = min(pair.end, u1);
-    const bool more = pair.next < u1;
+    const bool more = SHARE != 1 && pair.next < u1;
     after = pair;
     if (more) after = pair_at(pair.next);
-    const int pa0 = after.begin + wave;                         // this wave's first block there
+    const int pa0 = after.begin + turn;                         // this wave's first block there
     const bool ahead = more && pa0 < min(after.end, u1);
     const int b = pair.b, j = pair.j, N = pair.N;
     float M[RC], l[RC];
@@ -383,9 +389,9 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
       do {
         const int tile = block_at(pair, p, us, ue);
         // the wave's next block; behind the next pair, or the run: this one again
-        const bool on = p + kWaves < ue;
-        have = on ? p + kWaves : (ahead ? pa0 : -1);
-        const int block = on ? pair.block0 + block_at(pair, p + kWaves, us, ue)
+        const bool on = p + SHARE < ue;
+        have = on ? p + SHARE : (ahead ? pa0 : -1);
+        const int block = on ? pair.block0 + block_at(pair, p + SHARE, us, ue)
                              : (ahead ? after.block0 + block_at(after, pa0, after.begin, min(after.end, u1)) : pair.block0 + tile);
         // logits, four sums side by side: a sum's next product waits for the one before it
         floatx4 s[RC][4];
@@ -514,8 +520,24 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
               for (int v = 0; v < 4; ++v) acc[r][i0 + i][v] = fmaf(o[r][i][v], so[r][v], acc[r][i0 + i][v]);
         }
         load_values(block);
-        p += kWaves;
+        p += SHARE;
       } while (p < ue);
+    }
+    if (SHARE == 1) {
+#pragma unroll
+      for (int r = 0; r < RC; ++r) {
+        const float ls = rows_sum(l[r]), inv = ls == 0.f ? 0.f : 1.f / ls;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float to_out = __shfl(inv, 4 * kg + v);         // lane r holds row r
+          const int gr = set * ROWS + r * kKv8Rows + 4 * kg + v;
+          if (gr >= rows) continue;
+          float* dst = out + (((int64_t)b * n_q + gr / G) * hq + (int64_t)j * G + gr % G) * DH + col;
+#pragma unroll
+          for (int i = 0; i < NV; ++i) dst[16 * i] = acc[r][i][v] * to_out;
+        }
+      }
+      break;
     }
     if (!by_pair && us >= pair.end) {                           // the run begins in the room behind a pair
       if (!more) break;
@@ -645,6 +667,19 @@ bool one_workgroup_per_pair(const Problem& P, int sets, int64_t n_max) {
   const int blocks = groups >= 128 ? 8 * kWaves : 4 * kWaves;
   return n_max <= (int64_t)blocks * kKv8Block && groups <= 1 << 23;   // workgroups of a grid
 }
+// a wave for each pair where there are enough of them to fill the chip and the caches are
+// shorter still: nothing is merged, and the chip holds 2048 pairs at a time, not 512.  A
+// wave's blocks come one after the other (512 tokens take 18 us), so longer ones only where
+// there are many, or 32 query rows to merge.  In us, a workgroup / a wave per pair: 640
+// pairs of 512 tokens 20.8 / 17.3, 1024 of 200 22.3 / 15.5, of 512 30.9 / 24.8, of 1 to 512
+// 22.0 / 19.3; 2048 of 1024 98.8 / 85.4; 8192 of 64 83.8 / 40.1, of 1024 404 / 355; nine
+// query tokens over 1000, 640 sets of rows 57.3 / 42.0, 2048 154 / 93.5.  The other way: 512
+// pairs of 512 17.1 / 19.3, 1024 of 1 to 2000 52.7 / 57.2, nine query tokens, 512 sets 39.7 / 43.0
+bool one_wave_per_pair(const Problem& P, int n_q, int64_t n_max) {
+  const int64_t groups = (int64_t)P.B * P.hkv * row_sets(P, n_q);
+  const int blocks = groups >= 2048 || row_chunks(P, n_q) > 1 ? 16 : 8;
+  return groups >= 640 && n_max <= (int64_t)blocks * kKv8Block && one_workgroup_per_pair(P, row_sets(P, n_q), n_max);
+}
 // runs of a call over at most n_max tokens per sequence: a block for every wave at least
 int runs(const Problem& P, int n_q, int64_t n_max) {
   const int64_t blocks = (int64_t)P.B * P.hkv * pair_length((int)((n_max + kKv8Block - 1) / kKv8Block), 1 << 30);
@@ -671,18 +706,26 @@ hipError_t launch_kv8_decode(const Problem& P, const Kv8& C, int64_t n_max, cons
   float* part_o = (float*)ws;
   float* part_ml = part_o + part_rows * P.dh;
   const Seqs S{lengths, (int)n_max, P.B, P.hkv};
-  const dim3 grid((nwg + 7) / 8 * 8 * sets);
+  const bool by_wave = one_wave_per_pair(P, n_q, n_max);
+  const int wgs = by_wave ? (nwg + kWaves - 1) / kWaves : nwg;
+  const dim3 grid((wgs + 7) / 8 * 8 * sets);
   auto go = [&](auto elem, auto fmt, auto dh) {
     using T = decltype(elem);
-    auto with = [&](auto rc) {
-      hipLaunchKernelGGL((k_kv8_decode<T, fmt(), dh(), rc()>), grid, dim3(kWaves * 64), 0, st, (const T*)q, C.k_codes,
+    auto with = [&](auto rc, auto share) {
+      hipLaunchKernelGGL((k_kv8_decode<T, fmt(), dh(), rc(), share()>), grid, dim3(kWaves * 64), 0, st, (const T*)q, C.k_codes,
                          C.k_scales, C.v_codes, C.v_scales, part_ml, part_o, out, S, nwg, (int)by_pair, chunks, n_q,
                          P.G, kv8_tiles(P));
     };
+    auto by_share = [&](auto rc) {
+      if (by_wave)
+        with(rc, std::integral_constant<int, 1>());
+      else
+        with(rc, std::integral_constant<int, kWaves>());
+    };
     if (chunks == 1)
-      with(std::integral_constant<int, 1>());
+      by_share(std::integral_constant<int, 1>());
     else
-      with(std::integral_constant<int, 2>());
+      by_share(std::integral_constant<int, 2>());
   };
   auto by_fmt = [&](auto elem, auto dh) {
     if (C.format == S4R_KV_INT8)

@@ -129,7 +129,7 @@ class RefCache:
         return out
 
 
-def attention(cache, q, lengths):
+def attention(cache, q, lengths, waves=4):
     """q [B, n, hq, dh] float64 -> (out, tol): query token i of n sees lengths[b] - (n - 1 - i) tokens.
 
     tol bounds the fp32 kernel's error per (sequence, query, head).  With S = max_t sum_d |q_d k_td| / sqrt(dh): a
@@ -138,7 +138,7 @@ def attention(cache, q, lengths):
     factor, one of the difference to the maximum: at most 25 * 2^-24 S.  It changes a weight by that relative
     amount, and the sum by no more: 50 S.  exp2 is within 2^-22, twice: 8.  A lane adds 16 weights a block and a
     matrix instruction chain six roundings a block, over at most t blocks of one wave; weights of 22 bits, scale
-    and merges: 32 together.  All relative to sum p |v| / sum p <= max |v|."""
+    and merges: 32 together.  All relative to sum p |v| / sum p <= max |v|.  `waves` take a pair's blocks in turn."""
     B, n, hq, dh = q.shape
     G = hq // cache.H
     out, tol = np.zeros((B, n, hq, dh)), np.zeros((B, n, hq))
@@ -155,7 +155,7 @@ def attention(cache, q, lengths):
                 p = np.exp(z - z.max())
                 out[b, i, h] = p @ vv / p.sum()
                 S = (np.abs(kk) @ np.abs(q[b, i, h])).max() / np.sqrt(dh)
-                t = (N + BLOCK - 1) // BLOCK // 4 + 1
+                t = (N + BLOCK - 1) // BLOCK // waves + 1
                 tol[b, i, h] = (50 * S + 22 * t + 40) * 2.0 ** -24 * np.abs(vv).max()
     return out, tol
 

@@ -306,6 +306,71 @@ def test_more_sequences_than_lanes(n_max, given):
         assert np.all(np.abs(got[at] - want).max(-1) <= tol), n
 
 
+@pytest.mark.parametrize("fmt,dtype", [("int8", "bf16"), ("e4m3", "bf16"), ("int8", "fp32"), ("e4m3", "fp32")])
+@pytest.mark.parametrize("B,hq,hkv,dh,nq,n_max", [
+    (641, 4, 1, 128, 1, 512), (321, 8, 2, 64, 1, 300), (27, 48, 24, 64, 1, 65),         # a wave per pair just
+    (2050, 7, 1, 128, 1, 1024), (163, 28, 4, 128, 5, 1000), (330, 2, 2, 64, 17, 700),   # longer; 35 and 17 query rows
+    (107, 24, 3, 128, 16, 1024), (639, 2, 1, 128, 1, 512)])                              # four sets; a workgroup each
+def test_many_short_sequences(fmt, dtype, B, hq, hkv, dh, nq, n_max):
+    """As many (sequence, KV head) pairs as fill the chip.  Every sequence holds the same tokens up to its own length,
+    a dozen different ones from none to n_max in an order of their own."""
+    rng = np.random.default_rng(B + dh)
+    waves = 4 if B == 639 else 1                       # one less than fills it: a workgroup for each pair
+    cap = (n_max + 15) // 16 * 16
+    one = filled(rng, fmt, 1, hkv, dh, cap, [n_max], dtype)
+    c = cfg(B, hq, hkv, dh, cap, dtype)
+    t = {}
+    for s in "kv":
+        t[s + "_codes"] = torch.from_numpy(one.codes[s]).cuda().repeat(B, 1, 1, 1)
+        t[s + "_scales"] = torch.from_numpy(one.scales[s]).cuda().repeat(B, 1, 1)
+    cache = s4r.KV8Cache(fmt, **t)
+    known = [0, 1, 2, 63, 64, 65, 128, 129, n_max // 2, n_max - 1, n_max]
+    lengths = [known[i] for i in rng.integers(0, len(known), B)]
+    lengths[-1] = n_max
+    q = R.round_to(rng.standard_normal((1, nq, hq, dh)), dtype)
+    gq, ws = dev(np.tile(q, (B, 1, 1, 1)), c), s4r.alloc_kv8_workspace(c, nq)
+    out = torch.full((B, nq, hq, dh), float("nan"), device="cuda")
+    s4r.kv8_decode(c, cache, n_max, gq, ws, lengths=ints(lengths), out=out)
+    got = out.double().cpu().numpy()
+    for n in sorted(set(lengths)):
+        want, tol = R.attention(one, q, [min(n, n_max)], waves)              # what lies past the bound is not used
+        at = [b for b in range(B) if lengths[b] == n]
+        assert np.all(np.abs(got[at] - want).max(-1) <= tol), n
+    same_again = s4r.kv8_decode(c, cache, n_max, gq, ws, lengths=ints(lengths))
+    assert torch.equal(same_again, out)
+    whole = s4r.kv8_decode(c, cache, n_max, gq, ws).double().cpu().numpy()
+    want, tol = R.attention(one, q, [n_max], waves)
+    assert np.all(np.abs(whole - want).max(-1) <= tol)
+
+
+def test_many_short_sequences_in_a_graph():
+    """A captured call follows the lengths; a block that is not finite reaches its own pair only."""
+    B, hq, hkv, dh, n_max = 200, 8, 4, 128, 512
+    rng = np.random.default_rng(12)
+    held = [int(x) for x in rng.integers(1, n_max + 1, B)]
+    c = cfg(B, hq, hkv, dh, n_max)
+    cache = s4r.kv8_alloc(c, "int8")
+    x = torch.randn(2, B, n_max, hkv * dh, device="cuda").bfloat16()
+    s4r.kv8_write(c, cache, x[0], x[1])
+    q = torch.randn(B, 1, hq, dh, device="cuda").bfloat16()
+    ws, lengths, out = s4r.alloc_kv8_workspace(c), ints(held), torch.empty(B, 1, hq, dh, device="cuda")
+    s4r.kv8_decode(c, cache, n_max, q, ws, lengths=lengths, out=out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s4r.kv8_decode(c, cache, n_max, q, ws, lengths=lengths, out=out)
+    for turn in range(4):
+        lengths.copy_(ints([(n * (turn + 1)) % (n_max + 1) for n in held]))
+        cache.v_scales[7, 2, 0] = float("nan") if turn == 2 else 0.01
+        out.fill_(9)
+        g.replay()
+        eager = s4r.kv8_decode(c, cache, n_max, q, ws, lengths=lengths)
+        assert torch.equal(out.isnan(), eager.isnan()) and torch.equal(out.nan_to_num(), eager.nan_to_num())
+        bad = torch.zeros(B, 1, hq, dh, dtype=torch.bool, device="cuda")
+        bad[7, :, 4:6] = turn == 2 and int(lengths[7]) > 0
+        assert torch.equal(out.isnan(), bad)
+
+
 def test_agrees_with_the_bf16_cache():
     """Whole numbers up to 127 are the same values in both caches: the attention over them is the same but for fp32
     rounding (bound as in the reference; the bf16 cache's weights are fp32)."""
