@@ -134,9 +134,10 @@ __host__ __device__ inline int run_length(int total, int nwg) {
 struct Order {
   Seqs S;
   int shorter;                // pairs of fewer blocks than this have the room
+  int all;                    // the line's length
   int base;                   // the lanes hold sequences base .. base + 63
   int tok, mine, upto;        // this lane's sequence: tokens, its pairs' length, and the line up to its end
-  __device__ __forceinline__ explicit Order(const Seqs& s) : S(s), shorter(0) {}
+  __device__ __forceinline__ explicit Order(const Seqs& s) : S(s), shorter(0), all(0) {}
   __device__ __forceinline__ int length(int blocks) const { return pair_length(blocks, shorter); }
   __device__ __forceinline__ void load(int b0, int before) {
     const int b = b0 + (int)(threadIdx.x & 63);
@@ -162,7 +163,8 @@ struct Order {
     load(0, 0);
     shorter = (total() + nwg - 1) / nwg;
     place(0);
-    return run_length(total(), nwg);
+    all = total();
+    return run_length(all, nwg);
   }
   // the sequence at u (the lanes move on to it): its number, place and tokens
   __device__ __forceinline__ void find(int u, int& seq, int& begin, int& tokens) {
@@ -292,7 +294,7 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
   } else {
     const int run = order.lay_out(nwg);
     u0 = w * run;
-    u1 = min(u0 + run, order.total());
+    u1 = min(u0 + run, order.all);
     if (u0 >= u1) return;
     pair = pair_at(u0);
   }
@@ -590,21 +592,40 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
 }
 
 // merges the partials of the pairs that runs cut, and writes the zeros of sequences
-// without tokens.  One workgroup per query row of a sequence, groups of DH / 4
+// without tokens.  One workgroup per query row of a pair or, by_cut (more pairs than
+// runs), of a run: for the pair that begins in it and goes on behind it.  Groups of DH / 4
 // threads over the partials, each with its own running maximum (one round of loads).
+// Each of them works out the line, so fewer are better: both kernels, a workgroup for every
+// pair / every run: 3000 pairs of 1 to 200 tokens (N 2112) 136 / 62.5 us, 4096 of 64 (N
+// 4096) 107 / 66.9, 1024 of 4000 166.4 / 162.2
 template <int DH>
 __global__ __launch_bounds__(256) void k_kv8_combine(const float* __restrict__ part_ml, const float* __restrict__ part_o,
-                                                     float* __restrict__ out, Seqs S, int nwg, int chunks, int n_q,
-                                                     int G) {
+                                                     float* __restrict__ out, Seqs S, int nwg, int by_cut, int chunks,
+                                                     int n_q, int G) {
   constexpr int NG = 256 / (DH / 4);
-  const int gr = blockIdx.x, j = blockIdx.y, b = blockIdx.z;
-  const int t = threadIdx.x, g = t / (DH / 4), d4 = t % (DH / 4);
+  const int gr = blockIdx.x, t = threadIdx.x, g = t / (DH / 4), d4 = t % (DH / 4);
   const int hq = S.hkv * G;
-  float* dst = out + (((int64_t)b * n_q + gr / G) * hq + (int64_t)j * G + gr % G) * DH + 4 * d4;
+  auto row_of = [&](int b, int j) { return out + (((int64_t)b * n_q + gr / G) * hq + (int64_t)j * G + gr % G) * DH; };
   Order order(S);
   const int run = order.lay_out(nwg);
-  int begin, tokens;
-  order.of(b, begin, tokens);
+  int b = blockIdx.z, j = blockIdx.y, begin, tokens;
+  if (by_cut) {
+    const int w = blockIdx.y;
+    if (S.lengths) {
+      for (b = w; b < S.B; b += nwg) {
+        if (S.tokens(b)) continue;
+        for (int e = t; e < S.hkv * (DH / 4); e += 256)
+          *reinterpret_cast<floatx4*>(row_of(b, e / (DH / 4)) + e % (DH / 4) * 4) = floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+    }
+    const int end = (w + 1) * run;
+    if (end >= order.all) return;
+    order.find(end - 1, b, begin, tokens);
+    j = (end - 1 - begin) / order.length(blocks_of(tokens));
+  } else {
+    order.of(b, begin, tokens);
+  }
+  float* dst = row_of(b, j) + 4 * d4;
   const int T_b = blocks_of(tokens);
   if (T_b == 0) {
     if (g == 0) *reinterpret_cast<floatx4*>(dst) = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -613,6 +634,7 @@ __global__ __launch_bounds__(256) void k_kv8_combine(const float* __restrict__ p
   const int u0 = begin + j * order.length(T_b), u1 = u0 + T_b;
   const int w0 = u0 / run, w1 = (u1 - 1) / run;
   if (w0 == w1) return;                                         // finished by its run
+  if (by_cut && w0 != (int)blockIdx.y) return;                  // it began in an earlier one
   const int chunk = gr / kKv8Rows, row = gr % kKv8Rows;
   float M = -INFINITY, l = 0.f;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
@@ -751,11 +773,14 @@ hipError_t launch_kv8_decode(const Problem& P, const Kv8& C, int64_t n_max, cons
     const int length = pair_length(blocks, (pair_length(blocks, 0) * pairs + nwg - 1) / nwg);
     if (run_length(length * pairs, nwg) % length == 0) return hipSuccess;
   }
-  const dim3 cgrid(n_q * P.G, P.hkv, P.B);
+  const bool by_cut = (int64_t)P.B * P.hkv > nwg;
+  const dim3 cgrid(n_q * P.G, by_cut ? nwg : P.hkv, by_cut ? 1 : P.B);
   if (P.dh == 128)
-    hipLaunchKernelGGL(k_kv8_combine<128>, cgrid, dim3(256), 0, st, part_ml, part_o, out, S, nwg, chunks, n_q, P.G);
+    hipLaunchKernelGGL(k_kv8_combine<128>, cgrid, dim3(256), 0, st, part_ml, part_o, out, S, nwg, (int)by_cut, chunks, n_q,
+                       P.G);
   else
-    hipLaunchKernelGGL(k_kv8_combine<64>, cgrid, dim3(256), 0, st, part_ml, part_o, out, S, nwg, chunks, n_q, P.G);
+    hipLaunchKernelGGL(k_kv8_combine<64>, cgrid, dim3(256), 0, st, part_ml, part_o, out, S, nwg, (int)by_cut, chunks, n_q,
+                       P.G);
   return hipGetLastError();
 }
 

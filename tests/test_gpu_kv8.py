@@ -343,6 +343,49 @@ def test_many_short_sequences(fmt, dtype, B, hq, hkv, dh, nq, n_max):
     assert np.all(np.abs(whole - want).max(-1) <= tol)
 
 
+@pytest.mark.parametrize("fmt,dtype,B,hq,hkv,dh,nq", [
+    ("int8", "bf16", 300, 4, 1, 128, 1), ("e4m3", "fp32", 70, 16, 4, 64, 1), ("int8", "fp32", 65, 8, 4, 128, 9),
+    ("e4m3", "bf16", 131, 8, 1, 64, 16), ("int8", "bf16", 33, 32, 8, 128, 1), ("int8", "bf16", 40, 32, 8, 64, 9)])
+def test_more_pairs_than_runs(fmt, dtype, B, hq, hkv, dh, nq):
+    """A large bound and lengths from none to all of it: every cut pair is merged once, pairs over several runs among
+    them; sequences without tokens get zeros, also where none has any.  Captured, and replayed with other lengths."""
+    rng = np.random.default_rng(B)
+    cap = n_max = 2208
+    one = filled(rng, fmt, 1, hkv, dh, cap, [n_max], dtype)
+    c = cfg(B, hq, hkv, dh, cap, dtype)
+    t = {}
+    for s in "kv":
+        t[s + "_codes"] = torch.from_numpy(one.codes[s]).cuda().repeat(B, 1, 1, 1)
+        t[s + "_scales"] = torch.from_numpy(one.scales[s]).cuda().repeat(B, 1, 1)
+    cache = s4r.KV8Cache(fmt, **t)
+    known = [0, 1, 64, 129, 700, n_max]
+    want = {}
+    q = R.round_to(rng.standard_normal((1, nq, hq, dh)), dtype)
+    for n in known:
+        want[n] = R.attention(one, q, [n])
+    gq, ws = dev(np.tile(q, (B, 1, 1, 1)), c), s4r.alloc_kv8_workspace(c, nq)
+    ws.fill_(255)
+    out = torch.empty(B, nq, hq, dh, device="cuda")
+    sets = [[known[i] for i in rng.integers(0, len(known), B)],
+            [n_max if b in (0, 17, B - 1) else known[b % 3] for b in range(B)],      # a few long ones
+            [0] * B, [0] * (B - 1) + [n_max], [n_max] * B]
+    lengths = ints(sets[0])
+    s4r.kv8_decode(c, cache, n_max, gq, ws, lengths=lengths, out=out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s4r.kv8_decode(c, cache, n_max, gq, ws, lengths=lengths, out=out)
+    for these in sets:
+        lengths.copy_(ints(these))
+        out.fill_(float("nan"))
+        g.replay()
+        got = out.double().cpu().numpy()
+        for n in sorted(set(these)):
+            at = [b for b in range(B) if these[b] == n]
+            assert np.all(np.abs(got[at] - want[n][0]).max(-1) <= want[n][1]), n
+        assert torch.equal(s4r.kv8_decode(c, cache, n_max, gq, ws, lengths=lengths), out)
+
+
 def test_many_short_sequences_in_a_graph():
     """A captured call follows the lengths; a block that is not finite reaches its own pair only."""
     B, hq, hkv, dh, n_max = 200, 8, 4, 128, 512
