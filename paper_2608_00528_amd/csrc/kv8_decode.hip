@@ -16,9 +16,12 @@
 //    the values' into the addition of the block's sums;
 //  - a query row is scaled by a power of two to just below 2^15, where bf16 elements
 //    are fp16 numbers (exactly, down to 2^-28 of the row's largest) and fp32 ones two
-//    fp16 parts (22 bits); weights are kept at 2^9 to 2^15 for the largest and enter as
-//    two parts, 22 bits down to 2^-12 of the largest and 2^-33 of it in absolute terms.
-//    Their products with the codes are exact, sums are fp32.
+//    fp16 parts (22 bits);
+//  - softmax weights enter as three bf16 parts, all of their 24 bits and fp32's range: a
+//    token that holds nearly all the weight may have a value of zero (an attention sink),
+//    and the output is then made of weights far below the largest (two fp16 parts, the
+//    codes as fp16 there too, lost all of it at e^-23 and 3e-3 of it at e^-15).  Products
+//    with the codes are exact, sums are fp32.
 //
 // Work is split over one workgroup per CU by the tokens that are there: the blocks of
 // all (sequence, KV head) pairs in a row, an equal run of them for each workgroup, whose
@@ -41,7 +44,7 @@ namespace {
 constexpr int kWaves = 4;
 constexpr float kGrow = 6.f;            // the running maximum follows once a logit is 2^6 above it
 
-constexpr float kLift = 9.f;            // weights are exp2(logit - maximum + kLift)
+constexpr int kWeightParts = 3;         // bf16 parts of a softmax weight: all 24 bits, fp32's range
 constexpr int kQueryTop = 14;           // binary exponent of a query row's largest element in fp16
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -54,6 +57,18 @@ union Half8 {                           // an MFMA operand: eight fp16 values
 };
 __device__ __forceinline__ floatx4 mfma_f16(const Half8& a, const Half8& b, floatx4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0);
+}
+
+// the upper halves of two fp32 values: packed bf16, cut off
+__device__ __forceinline__ uint32_t upper2(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+// the same, and what is left of the values (exact)
+__device__ __forceinline__ uint32_t take_bf16x2(float& a, float& b) {
+  const uint32_t u = upper2(a, b);
+  a -= __uint_as_float(__float_as_uint(a) & 0xFFFF0000u);
+  b -= __uint_as_float(__float_as_uint(b) & 0xFFFF0000u);
+  return u;
 }
 
 // eight codes -> eight fp16 values (exact).  int8: a byte with its sign bit turned over
@@ -76,6 +91,24 @@ __device__ __forceinline__ Half8 codes_to_f16(uint32_t w0, uint32_t w1) {
     o.u[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.0f, true));
     o.u[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.0f, false));
     o.u[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.0f, true));
+  }
+  return o;
+}
+
+// the same eight codes as bf16 values (exact)
+template <int FMT>
+__device__ __forceinline__ Op8 codes_to_bf16(uint32_t w0, uint32_t w1) {
+  Op8 o;
+  if (FMT == S4R_KV_INT8) {
+    float a[4], b[4];
+    kv8_numbers<FMT>(w0, a);
+    kv8_numbers<FMT>(w1, b);
+    o.u = make_uint4(upper2(a[0], a[1]), upper2(a[2], a[3]), upper2(b[0], b[1]), upper2(b[2], b[3]));
+  } else {
+    o.u.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, false));
+    o.u.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, 1.0f, true));
+    o.u.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, false));
+    o.u.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, true));
   }
   return o;
 }
@@ -433,7 +466,7 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
             for (int i = 0; i < NV; ++i) vv[i][v] &= m;
           }
         }
-        Half8 pa[RC][2][2];
+        Op8 pa[RC][2][kWeightParts];
 #pragma unroll
         for (int r = 0; r < RC; ++r) {
 #pragma unroll
@@ -466,7 +499,7 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
               for (int i = 0; i < NV; ++i) acc[r][i][v] *= av;
             }
           }
-          const float ref = M[r] == -INFINITY ? 0.f : M[r] - kLift;
+          const float ref = M[r] == -INFINITY ? 0.f : M[r];
           float sum = 0.f;
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -476,16 +509,20 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
               sum += s[r][i][v];
             }
           l[r] += sum;
-          // two parts; contraction index 4 v + i of k-group kg
+          // contraction index 4 v + i of k-group kg
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h) {
+            uint32_t part[kWeightParts][4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int v = 2 * h + e / 2, i = 2 * (e % 2);
               float x = s[r][i][v], y = s[r][i + 1][v];
-              pa[r][h][0].u[e] = take_f16x2(x, y);
-              pa[r][h][1].u[e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(x, y));
+#pragma unroll
+              for (int p = 0; p < kWeightParts; ++p) part[p][e] = take_bf16x2(x, y);
             }
+#pragma unroll
+            for (int p = 0; p < kWeightParts; ++p) pa[r][h][p].u = make_uint4(part[p][0], part[p][1], part[p][2], part[p][3]);
+          }
         }
         // the block's scale; a row that sees none of its tokens takes no part, whatever it is
         float so[RC][4];
@@ -504,15 +541,15 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
             for (int i = 0; i < 4; ++i) o[r][i] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            Half8 bv[4];
+            Op8 bv[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) bv[i] = codes_to_f16<FMT>(vv[i0 + i][2 * h], vv[i0 + i][2 * h + 1]);
+            for (int i = 0; i < 4; ++i) bv[i] = codes_to_bf16<FMT>(vv[i0 + i][2 * h], vv[i0 + i][2 * h + 1]);
 #pragma unroll
             for (int r = 0; r < RC; ++r)
 #pragma unroll
-              for (int p = 0; p < 2; ++p)
+              for (int p = 0; p < kWeightParts; ++p)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[r][i] = mfma_f16(pa[r][h][p], bv[i], o[r][i]);
+                for (int i = 0; i < 4; ++i) o[r][i] = mfma16x16x32(pa[r][h][p], bv[i], o[r][i]);
           }
 #pragma unroll
           for (int r = 0; r < RC; ++r)
