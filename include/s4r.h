@@ -497,9 +497,8 @@ s4r_status s4r_kv8_read(const s4r_config* cfg, const s4r_kv8* cache, int64_t n_r
  * elements must be finite.  1 <= N <= capacity, 1 <= n_q and n_q * G <= 128.
  * ws: s4r_kv8_workspace_size bytes, 256-byte aligned (that of a larger n_q serves
  * too); its contents do not matter.
- * Sums are fp32.  The codes and the softmax weights (fp32) enter the matrix cores
- * exactly, and so do the elements of a bf16 query row down to 2^-28 of its largest; fp32
- * queries enter with 22 bits.
+ * Sums are fp32.  Codes, queries of either type (elements down to 2^-100 of their row's
+ * largest) and the softmax weights, which are fp32, enter the matrix cores exactly.
  */
 s4r_status s4r_kv8_workspace_size(const s4r_config* cfg, int32_t n_q, size_t* bytes);
 s4r_status s4r_kv8_decode(const s4r_config* cfg, const s4r_kv8* cache, int64_t N, const int32_t* lengths,

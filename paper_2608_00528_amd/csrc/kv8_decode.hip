@@ -8,20 +8,20 @@
 // 2 d_h bytes per token and KV head, so every other cost has to hide under the
 // stream:
 //  - the codes are operands as loaded (16 bytes per lane, 1 KiB per wave load) and
-//    become fp16 exactly; 16 or 32 query rows (query token x group member) share them;
+//    become bf16 exactly; 16 or 32 query rows (query token x group member) share them;
 //  - logits as K q^T: 16 tokens x 16 query rows per MFMA, so lane l ends with
 //    query row l % 16 and the tokens 16 i + 4 (l / 16) + v of the block - which is
 //    the A operand of P V, with no exchange between lanes;
 //  - scales are one number per block: the logits' goes into the exponent's factor,
 //    the values' into the addition of the block's sums;
-//  - a query row is scaled by a power of two to just below 2^15, where bf16 elements
-//    are fp16 numbers (exactly, down to 2^-28 of the row's largest) and fp32 ones two
-//    fp16 parts (22 bits);
+//  - bf16 queries are operands as they are, fp32 ones three bf16 parts, all of their 24
+//    bits (two fp16 parts kept 22: at logits of 64 a weight was off by 2.3e-5); a row is
+//    scaled by a power of two to below 1, so that its products with the codes stay finite;
 //  - softmax weights enter as three bf16 parts, all of their 24 bits and fp32's range: a
 //    token that holds nearly all the weight may have a value of zero (an attention sink),
-//    and the output is then made of weights far below the largest (two fp16 parts, the
-//    codes as fp16 there too, lost all of it at e^-23 and 3e-3 of it at e^-15).  Products
-//    with the codes are exact, sums are fp32.
+//    and the output is then made of weights far below the largest (two fp16 parts lost
+//    all of it at e^-23 and 3e-3 of it at e^-15).  Products with the codes are exact, sums
+//    are fp32.
 //
 // Work is split over one workgroup per CU by the tokens that are there: the blocks of
 // all (sequence, KV head) pairs in a row, an equal run of them for each workgroup, whose
@@ -43,21 +43,9 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr float kGrow = 6.f;            // the running maximum follows once a logit is 2^6 above it
-
-constexpr int kWeightParts = 3;         // bf16 parts of a softmax weight: all 24 bits, fp32's range
-constexpr int kQueryTop = 14;           // binary exponent of a query row's largest element in fp16
+constexpr int kWeightParts = 3;         // bf16 parts of a softmax weight
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-union Half8 {                           // an MFMA operand: eight fp16 values
-  u32x4 u;
-  f16x2 p[4];
-  f16x8 v;
-};
-__device__ __forceinline__ floatx4 mfma_f16(const Half8& a, const Half8& b, floatx4 c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a.v, b.v, c, 0, 0, 0);
-}
 
 // the upper halves of two fp32 values: packed bf16, cut off
 __device__ __forceinline__ uint32_t upper2(float a, float b) {
@@ -71,31 +59,7 @@ __device__ __forceinline__ uint32_t take_bf16x2(float& a, float& b) {
   return u;
 }
 
-// eight codes -> eight fp16 values (exact).  int8: a byte with its sign bit turned over
-// behind 0x64 is the fp16 number 1024 + 128 + code
-template <int FMT>
-__device__ __forceinline__ Half8 codes_to_f16(uint32_t w0, uint32_t w1) {
-  Half8 o;
-  if (FMT == S4R_KV_INT8) {
-    w0 ^= 0x80808080u;
-    w1 ^= 0x80808080u;
-    o.u[0] = __builtin_amdgcn_perm(0x64646464u, w0, 0x04010400u);
-    o.u[1] = __builtin_amdgcn_perm(0x64646464u, w0, 0x04030402u);
-    o.u[2] = __builtin_amdgcn_perm(0x64646464u, w1, 0x04010400u);
-    o.u[3] = __builtin_amdgcn_perm(0x64646464u, w1, 0x04030402u);
-    const f16x2 zero = {(_Float16)1152.f, (_Float16)1152.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o.p[i] -= zero;
-  } else {
-    o.u[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.0f, false));
-    o.u[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w0, 1.0f, true));
-    o.u[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.0f, false));
-    o.u[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w1, 1.0f, true));
-  }
-  return o;
-}
-
-// the same eight codes as bf16 values (exact)
+// eight codes -> eight bf16 values (exact)
 template <int FMT>
 __device__ __forceinline__ Op8 codes_to_bf16(uint32_t w0, uint32_t w1) {
   Op8 o;
@@ -111,14 +75,6 @@ __device__ __forceinline__ Op8 codes_to_bf16(uint32_t w0, uint32_t w1) {
     o.u.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, 1.0f, true));
   }
   return o;
-}
-
-// two fp32 values as fp16, cut off, and what is left of them
-__device__ __forceinline__ uint32_t take_f16x2(float& a, float& b) {
-  const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
-  a -= (float)h[0];
-  b -= (float)h[1];
-  return __builtin_bit_cast(uint32_t, h);
 }
 
 // max / sum over the four lanes l, l ^ 16, l ^ 32, l ^ 48
@@ -227,7 +183,7 @@ struct Order {
   }
 };
 
-// eight query elements as fp32; fp16 parts that hold them
+// eight query elements as fp32; bf16 parts that hold them
 template <typename T>
 struct Query;
 template <>
@@ -244,7 +200,7 @@ struct Query<uint16_t> {
 };
 template <>
 struct Query<float> {
-  static constexpr int parts = 2;
+  static constexpr int parts = 3;
   __device__ __forceinline__ static void load(const float* p, float* x) {
     const floatx4 a = *reinterpret_cast<const floatx4*>(p), b = *reinterpret_cast<const floatx4*>(p + 4);
 #pragma unroll
@@ -262,9 +218,11 @@ __device__ __forceinline__ int64_t part_row(int slot, int chunks, int chunk, int
 // RC: chunks of 16 query rows that a workgroup works on; they share its blocks and
 // their conversion.  SHARE: waves that take a pair's blocks in turn - the workgroup's, or
 // 1: a pair to each wave, nothing to merge, and a workgroup's waves never wait for each
-// other (one_wave_per_pair)
+// other (one_wave_per_pair).  Two workgroups' registers fit a CU but for fp32 queries over
+// 128 dims, whose parts take 264: held to 256, 8 x 16256 tokens of 8 KV heads take 57 us, not
+// 51, and 512 pairs of 512 tokens 21.5, not 20.5
 template <typename T, int FMT, int DH, int RC, int SHARE>
-__global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
+__global__ __launch_bounds__(kWaves * 64, RC == 1 && (sizeof(T) == 2 || DH == 64) ? 2 : 1) void k_kv8_decode(
     const T* __restrict__ q, const uint8_t* __restrict__ k_codes, const float* __restrict__ k_scales,
     const uint8_t* __restrict__ v_codes, const float* __restrict__ v_scales, float* __restrict__ part_ml,
     float* __restrict__ part_o, float* __restrict__ out, Seqs S, int nwg, int by_pair, int chunks, int n_q, int G,
@@ -389,7 +347,7 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
         load_keys(block);
         load_values(block);
       }
-      Half8 qb[RC][KB][2][NP];
+      Op8 qb[RC][KB][2][NP];
       float fq[RC];                                             // a row's power of two with 1 / sqrt(d_h) and log2 e
 #pragma unroll
       for (int r = 0; r < RC; ++r) {
@@ -408,17 +366,20 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
         int up;                                                 // largest element in [1/2, 1) * 2^up
         (void)frexpf(top, &up);
         up = top > 0.f && top < INFINITY ? up : 0;
-        fq[r] = ldexpf(to_log2, up - 1 - kQueryTop);
+        fq[r] = ldexpf(to_log2, up);
 #pragma unroll
         for (int d = 0; d < KB; ++d)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[d][h][e] = ldexpf(x[d][h][e], kQueryTop + 1 - up);
+            for (int e = 0; e < 8; ++e) x[d][h][e] = ldexpf(x[d][h][e], -up);
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
+            for (int p = 0; p < NP; ++p) {
+              uint32_t u[4];
 #pragma unroll
-              for (int e = 0; e < 4; ++e) qb[r][d][h][p].u[e] = take_f16x2(x[d][h][2 * e], x[d][h][2 * e + 1]);
+              for (int e = 0; e < 4; ++e) u[e] = take_bf16x2(x[d][h][2 * e], x[d][h][2 * e + 1]);
+              qb[r][d][h][p].u = make_uint4(u[0], u[1], u[2], u[3]);
+            }
           }
       }
       do {
@@ -438,15 +399,15 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 ? 2 : 1) void k_kv8_decode(
         for (int d = 0; d < KB; ++d)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            Half8 a[4];
+            Op8 a[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = codes_to_f16<FMT>(kk[i * KB + d][2 * h], kk[i * KB + d][2 * h + 1]);
+            for (int i = 0; i < 4; ++i) a[i] = codes_to_bf16<FMT>(kk[i * KB + d][2 * h], kk[i * KB + d][2 * h + 1]);
 #pragma unroll
             for (int r = 0; r < RC; ++r)
 #pragma unroll
               for (int p = 0; p < NP; ++p)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[r][i] = mfma_f16(a[i], qb[r][d][h][p], s[r][i]);
+                for (int i = 0; i < 4; ++i) s[r][i] = mfma16x16x32(a[i], qb[r][d][h][p], s[r][i]);
           }
         float f[RC];
 #pragma unroll

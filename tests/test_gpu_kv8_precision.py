@@ -63,3 +63,37 @@ def test_first_token_holds_the_weight_and_no_value(fmt, dtype, hq, hkv, dh, nq, 
                          s4r.alloc_kv8_workspace(c, nq), lengths=ints([n] * copies)).double().cpu().numpy()
     err = np.abs(got - want)
     assert np.all(err <= tol), f"worst {(err / np.maximum(tol, 1e-300)).max():.3g} of the bound"
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("copies,cap", [(1, 64), (1, 4096), (640, 64)])
+def test_fp32_queries_keep_their_last_bits(fmt, dh, copies, cap):
+    """Four query heads that differ in their last two bits alone: c (1 + 2^-11 + i 2^-23).  The one key element that
+    they meet is a power of two after its scale, so a logit is the query's element times a power of two, exactly:
+    Z (1 + 2^-11 + i 2^-23), Z = 64 or 45 nats above the second token's, whose value alone is not zero.  The output
+    is exp(-logit): head i is off head 0 by i Z 2^-23 in the exponent.  Roundings, in each head: the logit's last
+    factor (2^-24 Z), exp2 (its own 2^-22), the sum and the division (below 2^-22 together)."""
+    hq, n = 4, 2
+    q = np.zeros((1, 1, hq, dh))
+    q[0, 0, :, 0] = 8 * (1 + 2.0 ** -11 + np.arange(hq) * 2.0 ** -23)
+    q = R.round_to(q, "fp32")
+    assert np.array_equal(q[0, 0, :, 0] / q[0, 0, 0, 0] > 1, np.arange(hq) > 0)
+    x = {s: np.zeros((1, n, 1, dh)) for s in "kv"}
+    x["k"][0, 0, 0, 0], x["k"][0, 0, 0, 1] = 64, 127
+    x["v"][0, 1] = 1
+    ref = R.RefCache(fmt, 1, 1, dh, cap)
+    ref.write({s: x[s].reshape(1, n, dh) for s in "kv"}, [0], [n])
+    logit = 64 * q[0, 0, :, 0] / np.sqrt(dh)
+    assert logit[0] > 40
+    c = cfg(copies, hq, 1, dh, cap, "fp32")
+    t = {}
+    for s in "kv":
+        t[s + "_codes"] = torch.from_numpy(ref.codes[s]).cuda().repeat(copies, 1, 1, 1)
+        t[s + "_scales"] = torch.from_numpy(ref.scales[s]).cuda().repeat(copies, 1, 1)
+    got = s4r.kv8_decode(c, s4r.KV8Cache(fmt, **t), cap, dev(np.tile(q, (copies, 1, 1, 1)), c),
+                         s4r.alloc_kv8_workspace(c), lengths=ints([n] * copies)).double().cpu().numpy()
+    assert np.all(got > 0)
+    apart = np.log(got / got[:, :, :1])
+    want = -(logit - logit[0])[:, None]
+    assert np.all(np.abs(apart - want) <= logit[0] * 2.0 ** -23 + 2 * 2.0 ** -21)
