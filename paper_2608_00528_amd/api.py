@@ -7,6 +7,7 @@ the gfx950 kernels of libs4r.so; there is no CPU path.
 """
 
 import ctypes
+import math
 
 import torch
 
@@ -417,23 +418,51 @@ def _here(t, name, dev):
         raise ValueError(f"{name} is on {t.device}, not on the current device {dev}")
 
 
-def _rows(t, name, dtype, width, dev):
-    """(address, rows, elements between rows) of a GPU tensor [..., heads, head_dim] or [..., width] whose last
-    axes are packed to rows of `width` and whose leading axes step evenly from row to row."""
+def _batch_first(shape, name, batch, width):
+    """The rows of `width` elements in `shape` come sequence by sequence: leading axes that make up the batch, or
+    rows in one axis (sequence b's before b + 1's)."""
+    if shape[0] == batch:
+        return
+    rows = math.prod(shape) // width
+    if rows == batch or batch == 1:
+        return
+    n = 1
+    for a in shape:
+        if a == 1:
+            continue
+        if n == 1 and a % rows == 0:
+            return
+        n *= a
+        if n >= batch:
+            break
+    if n != batch:
+        raise ValueError(f"{name} has shape {tuple(shape)}: the {batch} sequences of the batch were expected first")
+
+
+def _heads_last(shape, name, heads, dh):
+    """The last axis holds whole heads: rows of heads * dh elements, or heads of dh."""
+    if not shape or shape[-1] % dh:
+        raise ValueError(f"{name} has shape {tuple(shape)}: rows of {heads} heads of {dh} elements were expected")
+
+
+def _rows(t, name, dtype, heads, dh, dev):
+    """(address, rows, elements between rows) of a GPU tensor [..., heads, dh] or [..., heads * dh] whose last
+    axes are packed to rows and whose leading axes step evenly from row to row."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
     _here(t, name, dev)
-    shape = t.shape
+    shape, width = t.shape, heads * dh
     d = len(shape)
     # the usual cases first: a packed tensor, one leading axis
     if d > 1:
         lead = d - 1 if shape[-1] == width else d - 2
-        if lead == d - 1 or shape[-1] * shape[-2] == width:
+        if lead == d - 1 or (shape[-1] == dh and shape[-2] == heads):
             n = t.numel()
             if n and t.is_contiguous():
                 return t.data_ptr(), n // width, width
+    _heads_last(shape, name, heads, dh)
     strides, n = t.stride(), 1
     while d and n < width:
         d -= 1
@@ -480,7 +509,7 @@ def qk_norm_rope(cfg, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, q
             args += (None, 0, None, 0)
             outs.append(None)
             continue
-        p, rows, stride = _rows(x, name, dt, heads * dh, dev)
+        p, rows, stride = _rows(x, name, dt, heads, dh, dev)
         if n is not None and rows != n:
             raise ValueError(f"q has {n} tokens and k {rows}")
         n = rows
@@ -488,7 +517,7 @@ def qk_norm_rope(cfg, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, q
             o = x.new_empty(x.shape)
             args += (p, stride, o.data_ptr(), heads * dh)
         else:
-            po, ro, so = _rows(o, name + "_out", dt, heads * dh, dev)
+            po, ro, so = _rows(o, name + "_out", dt, heads, dh, dev)
             if ro != n:
                 raise ValueError(f"{name}_out has {ro} tokens, expected {n}")
             args += (p, stride, po, so)
@@ -592,17 +621,20 @@ def _kv8(cfg, cache, dev):
 
 
 def kv8_write(cfg, cache, k, v, row0=0, starts=None, counts=None):
-    """Quantise rows k, v [B, n, h_kv d_h] (or [B, n, h_kv, d_h]; evenly spaced rows) into the cache as tokens
+    """Quantise rows k, v [B, n, h_kv d_h] (or [B, n, h_kv, d_h]; evenly spaced rows; B and n may be one axis) into
+    the cache as tokens
     starts[b] + i (int32 GPU tensor; row0 + i without it) for i < counts[b] (all without it).  A sequence whose range
     does not fit is left as it is."""
-    dt, width = storage_dtype(cfg), cfg.n_kv_heads * cfg.head_dim
+    dt, heads, dh = storage_dtype(cfg), cfg.n_kv_heads, cfg.head_dim
     dev = _device()
     c = _kv8(cfg, cache, dev)
-    pk, rows, sk = _rows(k, "k", dt, width, dev)
-    pv, rv, sv = _rows(v, "v", dt, width, dev)
+    pk, rows, sk = _rows(k, "k", dt, heads, dh, dev)
+    pv, rv, sv = _rows(v, "v", dt, heads, dh, dev)
     if rows != rv or rows % cfg.batch:
         raise ValueError(f"k has {rows} rows and v {rv}: a multiple of the batch {cfg.batch}, the same for both, "
                          "was expected")
+    _batch_first(k.shape, "k", cfg.batch, heads * dh)
+    _batch_first(v.shape, "v", cfg.batch, heads * dh)
     L.check(L.load().s4r_kv8_write(_cfgp(cfg), c, rows // cfg.batch, row0, _ints(starts, "starts", cfg.batch, dev),
                                    _ints(counts, "counts", cfg.batch, dev), pk, sk, pv, sv, _stream()))
 

@@ -1,0 +1,45 @@
+"""Axes of the tensors around the 8-bit KV cache: rows that come in another order than the library takes them
+are refused, whatever the number of elements; the same order in other axes is taken."""
+
+import pytest
+import torch
+
+import paper_2608_00528_amd as s4r
+from tests.test_gpu_kv8 import cfg, ints
+
+pytestmark = pytest.mark.gpu
+
+B, N, HQ, HKV, DH, CAP = 2, 3, 6, 3, 64, 128
+
+
+def rand(*shape, dtype=torch.bfloat16):
+    return torch.randn(*shape, device="cuda").to(dtype)
+
+
+def refused(call, text):
+    with pytest.raises((ValueError, s4r.S4RError), match=text):
+        call()
+
+
+def test_rows_written_sequence_by_sequence():
+    c = cfg(B, HQ, HKV, DH, CAP)
+    k, v = rand(B, N, HKV, DH), rand(B, N, HKV, DH)
+    cache = s4r.kv8_alloc(c)
+    s4r.kv8_write(c, cache, k, v)
+    held = s4r.kv8_read(c, cache, N)
+    for x in (k.transpose(0, 1).contiguous(), k.transpose(0, 1), k.transpose(0, 1).flatten(2)):
+        refused(lambda: s4r.kv8_write(c, cache, x, v), "sequences|evenly")
+        refused(lambda: s4r.kv8_write(c, cache, k, x), "sequences|evenly")
+    # the elements of a head in the axis before the heads
+    refused(lambda: s4r.kv8_write(c, cache, k.transpose(2, 3).contiguous(), v), "expected")
+    assert all(torch.equal(a, b) for a, b in zip(held, s4r.kv8_read(c, cache, N)))
+    # the same rows in other axes
+    for shape in ((B * N, HKV, DH), (B * N, HKV * DH), (B, 1, N, HKV * DH), (B, N, HKV, 1, DH)):
+        other = s4r.kv8_alloc(c)
+        s4r.kv8_write(c, other, k.view(shape), v.view(shape))
+        assert all(torch.equal(a, b) for a, b in zip(held, s4r.kv8_read(c, other, N)))
+    # one sequence, and one row of each
+    one = cfg(1, HQ, HKV, DH, CAP)
+    s4r.kv8_write(one, s4r.kv8_alloc(one), k.flatten(0, 1), v)
+    four = cfg(4, HQ, HKV, DH, CAP)
+    s4r.kv8_write(four, s4r.kv8_alloc(four), rand(2, 2, HKV, DH), rand(4, HKV * DH), row0=9)
