@@ -671,6 +671,12 @@ def alloc_kv8_workspace(cfg, n_queries=1, device="cuda"):
     return torch.empty(kv8_workspace_size(cfg, n_queries), dtype=torch.uint8, device=device)
 
 
+def _queries(t, name, cfg):
+    """Query tokens of every sequence, [B, n, h_q, d_h] or the same with some of these axes as one."""
+    _heads_last(t.shape, name, cfg.n_q_heads, cfg.head_dim)
+    _batch_first(t.shape, name, cfg.batch, cfg.n_q_heads * cfg.head_dim)
+
+
 def kv8_decode(cfg, cache, n_tokens, q, ws, lengths=None, out=None):
     """Attention of the newest query tokens q [B, h_q, d_h] or [B, n, h_q, d_h] (rotated as the cached keys are)
     over the 8-bit cache: tokens 0 .. n_tokens - 1 of every sequence, or of lengths[b] (int32 GPU tensor, at most
@@ -684,10 +690,14 @@ def kv8_decode(cfg, cache, n_tokens, q, ws, lengths=None, out=None):
     _here(q, "q", dev)
     if q.numel() == 0 or q.numel() % per:
         raise ValueError(f"q has shape {tuple(q.shape)}: [batch, n, n_q_heads, head_dim] was expected")
+    if q.shape[0] != cfg.batch or q.shape[-1] != cfg.head_dim:
+        _queries(q, "q", cfg)
     if out is None:
         out = q.new_empty(q.shape, dtype=torch.float32)
     elif out.numel() != q.numel():
         raise ValueError(f"out has {out.numel()} elements, expected {q.numel()}")
+    elif out.shape != q.shape:
+        _queries(out, "out", cfg)
     po, pw = _ptr(out, "out", torch.float32), _ptr(ws, "ws", torch.uint8)
     _here(out, "out", dev)
     _here(ws, "ws", dev)

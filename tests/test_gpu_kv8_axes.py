@@ -43,3 +43,26 @@ def test_rows_written_sequence_by_sequence():
     s4r.kv8_write(one, s4r.kv8_alloc(one), k.flatten(0, 1), v)
     four = cfg(4, HQ, HKV, DH, CAP)
     s4r.kv8_write(four, s4r.kv8_alloc(four), rand(2, 2, HKV, DH), rand(4, HKV * DH), row0=9)
+
+
+def test_query_tokens_sequence_by_sequence():
+    c = cfg(B, HQ, HKV, DH, CAP)
+    cache, ws = s4r.kv8_alloc(c), s4r.alloc_kv8_workspace(c, N)
+    s4r.kv8_write(c, cache, rand(B, 100, HKV, DH), rand(B, 100, HKV, DH))
+    q = rand(B, N, HQ, DH)
+    want = s4r.kv8_decode(c, cache, 100, q, ws)
+    turned = q.transpose(0, 1).contiguous()
+    refused(lambda: s4r.kv8_decode(c, cache, 100, turned, ws), "sequences")
+    refused(lambda: s4r.kv8_decode(c, cache, 100, q.transpose(2, 3).contiguous(), ws), "expected")
+    out = torch.full((N, B, HQ, DH), 7.0, device="cuda")
+    refused(lambda: s4r.kv8_decode(c, cache, 100, q, ws, out=out), "sequences")
+    refused(lambda: s4r.kv8_decode(c, cache, 100, q, ws, out=out.view(B, N, DH, HQ)), "expected")
+    assert bool((out == 7).all())
+    # the same rows in other axes
+    for shape in ((B * N, HQ, DH), (B, N * HQ, DH), (B, N, HQ * DH), (B, N, HKV, HQ // HKV, DH), (B * N * HQ * DH,)):
+        got = s4r.kv8_decode(c, cache, 100, q.view(shape), ws)
+        assert got.shape == shape and torch.equal(got.view_as(want), want)
+        got = s4r.kv8_decode(c, cache, 100, q, ws, out=torch.empty(shape, device="cuda"))
+        assert got.shape == shape and torch.equal(got.view_as(want), want)
+    one = s4r.kv8_decode(c, cache, 98, q[:, 0].contiguous(), ws)
+    assert one.shape == (B, HQ, DH) and torch.equal(one, want[:, 0])
