@@ -478,7 +478,8 @@ s4r_status s4r_kv8_write(const s4r_config* cfg, const s4r_kv8* cache, int64_t n_
  * Rows out of the cache: k_out, v_out [B, n_rows, h_kv * d_h] in the storage
  * dtype (code * scale in fp32, rounded once), row i of sequence b the token
  * first_b + i as above; rows from counts[b] on are zeros, and so are all rows
- * of a sequence whose range does not lie in [0, capacity).
+ * of a sequence whose range does not lie in [0, capacity).  k_out and v_out must not
+ * overlap.
  */
 s4r_status s4r_kv8_read(const s4r_config* cfg, const s4r_kv8* cache, int64_t n_rows, int64_t row0,
                         const int32_t* starts, const int32_t* counts, void* k_out, void* v_out,

@@ -652,6 +652,9 @@ def kv8_read(cfg, cache, n_rows, row0=0, starts=None, counts=None, k=None, v=Non
             t = cache.k_codes.new_empty(shape, dtype=dt)
         elif t.numel() != shape[0] * shape[1] * shape[2]:
             raise ValueError(f"{name} has {t.numel()} elements, expected {shape}")
+        elif t.shape != shape:
+            _heads_last(t.shape, name, cfg.n_kv_heads, cfg.head_dim)
+            _batch_first(t.shape, name, cfg.batch, shape[2])
         out.append(t)
     ptrs = [_ptr(t, name, dt) for t, name in zip(out, "kv")]
     for t, name in zip(out, "kv"):

@@ -590,6 +590,9 @@ s4r_status s4r_kv8_read(const s4r_config* cfg, const s4r_kv8* cache, int64_t n_r
   if ((st = make_kv8(P, cache, C)) || (st = kv8_range(P, C, n_rows, row0, starts, counts))) return st;
   S4R_REQ(k_out);
   S4R_REQ(v_out);
+  const uintptr_t ka = (uintptr_t)k_out, va = (uintptr_t)v_out;
+  if ((ka > va ? ka - va : va - ka) < (uint64_t)P.B * n_rows * P.Dp * elem_size(P))
+    return fail(S4R_ERR_BAD_SHAPE, "k_out and v_out overlap");
   return hip_status(launch_kv8_read(P, C, n_rows, k_out, v_out, stream), "s4r_kv8_read launch");
 }
 

@@ -66,3 +66,25 @@ def test_query_tokens_sequence_by_sequence():
         assert got.shape == shape and torch.equal(got.view_as(want), want)
     one = s4r.kv8_decode(c, cache, 98, q[:, 0].contiguous(), ws)
     assert one.shape == (B, HQ, DH) and torch.equal(one, want[:, 0])
+
+
+def test_rows_read_into_two_tensors_sequence_by_sequence():
+    c = cfg(B, HQ, HKV, DH, CAP)
+    cache = s4r.kv8_alloc(c)
+    s4r.kv8_write(c, cache, rand(B, N, HKV, DH), rand(B, N, HKV, DH))
+    k, v = s4r.kv8_read(c, cache, N)
+    a = torch.zeros(2, B, N, HKV * DH, dtype=torch.bfloat16, device="cuda")
+    refused(lambda: s4r.kv8_read(c, cache, N, k=a[0], v=a[0]), "overlap")
+    flat = a.flatten()
+    n = k.numel()
+    refused(lambda: s4r.kv8_read(c, cache, N, k=flat[:n], v=flat[n - 8:2 * n - 8]), "overlap")
+    refused(lambda: s4r.kv8_read(c, cache, N, k=flat[n - 8:2 * n - 8], v=flat[:n]), "overlap")
+    refused(lambda: s4r.kv8_read(c, cache, N, k=a[0].view(N, B, HKV * DH)), "sequences")
+    refused(lambda: s4r.kv8_read(c, cache, N, v=a[0].view(B, N, DH, HKV)), "expected")
+    assert not a.any()
+    # side by side, and the same rows in other axes
+    s4r.kv8_read(c, cache, N, k=a[1], v=a[0])
+    assert torch.equal(a[1], k) and torch.equal(a[0], v)
+    a.zero_()
+    s4r.kv8_read(c, cache, N, k=flat[:n], v=a[1].view(B * N, HKV, DH))
+    assert torch.equal(a[0], k) and torch.equal(a[1], v)
