@@ -494,14 +494,42 @@ def _ints(t, name, n, dev):
     return p
 
 
+def _same_order(a, b, names):
+    """Axes a and b of as many elements count them in the same order: they are equal, or one's are the other's with
+    some of them as one."""
+    if a == b:
+        return
+    ends = []
+    for shape in (a, b):
+        n, e = 1, {1}
+        for x in shape:
+            n *= x
+            e.add(n)
+        ends.append(e)
+    if not (ends[0] <= ends[1] or ends[1] <= ends[0]):
+        raise ValueError(f"{names} have axes {tuple(a)} and {tuple(b)}")
+
+
+def _tokens(t, heads, dh):
+    """The axes of a tensor's rows where they are several."""
+    shape = t.shape
+    d, n = len(shape), 1
+    if d < 3 or (d == 3 and shape[-1] == dh and shape[-2] == heads):
+        return None
+    while d and n < heads * dh:
+        d -= 1
+        n *= shape[d]
+    return shape[:d]
+
+
 def qk_norm_rope(cfg, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, q_out=None, k_out=None):
-    """Query heads q [..., h_q, d_h] and key heads k [..., h_kv, d_h] of the same tokens, each head normalised
-    (x / sqrt(mean(x^2) + eps) * weight [d_h]; not where its weight is None) and rotated by its token's position
+    """Query heads q [..., h_q, d_h] and key heads k [..., h_kv, d_h] of the same tokens in the same order, each head
+    normalised (x / sqrt(mean(x^2) + eps) * weight [d_h]; not where its weight is None) and rotated by its token's position
     (int32, one per token; rope_theta = 0: not rotated, positions may be None).  q or k may be None.  The tokens may
     be slices of a fused projection's rows; outputs (new packed tensors by default) may be the inputs themselves.
     Returns (q_out, k_out)."""
     dt, dh, dev, n = storage_dtype(cfg), cfg.head_dim, _device(), None
-    args, outs = [], []
+    args, outs, axes = [], [], None
     for name, x, o, heads in (("q", q, q_out, cfg.n_q_heads), ("k", k, k_out, cfg.n_kv_heads)):
         if x is None:
             if o is not None:
@@ -512,7 +540,11 @@ def qk_norm_rope(cfg, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, q
         p, rows, stride = _rows(x, name, dt, heads, dh, dev)
         if n is not None and rows != n:
             raise ValueError(f"q has {n} tokens and k {rows}")
-        n = rows
+        n, own = rows, _tokens(x, heads, dh)
+        if own is not None:
+            if axes is not None:
+                _same_order(axes, own, "the tokens of q and k")
+            axes = own
         if o is None:
             o = x.new_empty(x.shape)
             args += (p, stride, o.data_ptr(), heads * dh)
@@ -520,12 +552,18 @@ def qk_norm_rope(cfg, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, q
             po, ro, so = _rows(o, name + "_out", dt, heads, dh, dev)
             if ro != n:
                 raise ValueError(f"{name}_out has {ro} tokens, expected {n}")
+            to = _tokens(o, heads, dh)
+            if own is not None and to is not None:
+                _same_order(own, to, f"the tokens of {name} and {name}_out")
             args += (p, stride, po, so)
         outs.append(o)
     if n is None:
         raise ValueError("q or k is required")
     if q_out is not None or k_out is not None:
         _apart(args, n, cfg, dt)
+    pos = _ints(positions, "positions", n, dev)
+    if pos is not None and axes is not None:
+        _same_order(axes, positions.shape, "the tokens and positions")
     weights = []
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         weights.append(_ptr(w, name, dt, False))
@@ -535,7 +573,7 @@ def qk_norm_rope(cfg, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, q
                 raise ValueError(f"{name} has {w.numel()} entries, expected {dh}")
     L.check(L.load().s4r_qk_norm_rope(
         _cfgp(cfg), n, args[0], args[1], args[4], args[5], weights[0], weights[1], eps,
-        _ints(positions, "positions", n, dev), args[2], args[3], args[6], args[7], _stream()))
+        pos, args[2], args[3], args[6], args[7], _stream()))
     return tuple(outs)
 
 

@@ -88,3 +88,27 @@ def test_rows_read_into_two_tensors_sequence_by_sequence():
     a.zero_()
     s4r.kv8_read(c, cache, N, k=flat[:n], v=a[1].view(B * N, HKV, DH))
     assert torch.equal(a[0], k) and torch.equal(a[1], v)
+
+
+def test_heads_of_the_same_tokens():
+    c = s4r.make_config(batch=1, n_q_heads=HQ, n_kv_heads=HKV, head_dim=DH, rank=32, capacity=64, rope_theta=1e4)
+    q, k = rand(B, N, HQ, DH), rand(B, N, HKV, DH)
+    pos = ints(range(B * N)).view(B, N)
+    want = s4r.qk_norm_rope(c, q, k, pos)
+    refused(lambda: s4r.qk_norm_rope(c, q, k.transpose(0, 1).contiguous(), pos), "axes")
+    refused(lambda: s4r.qk_norm_rope(c, q, k, pos.t().contiguous()), "axes")
+    refused(lambda: s4r.qk_norm_rope(c, q, None, pos.t().contiguous()), "axes")
+    refused(lambda: s4r.qk_norm_rope(c, q.transpose(2, 3).contiguous(), k, pos), "expected")
+    out = torch.zeros(N, B, HQ, DH, dtype=torch.bfloat16, device="cuda")
+    refused(lambda: s4r.qk_norm_rope(c, q, k, pos, q_out=out), "axes")
+    refused(lambda: s4r.qk_norm_rope(c, q, k, pos, q_out=out.view(B, N, DH, HQ)), "expected")
+    assert not out.any()
+    # the same tokens in other axes
+    for a, b, p in ((q.flatten(0, 1), k, pos), (q, k.flatten(0, 1), pos.flatten()), (q.flatten(2), k.flatten(2), pos),
+                    (q.view(B, N, HKV, HQ // HKV, DH), k.view(B, 1, N, HKV, DH), pos.view(1, B, N)),
+                    (q.flatten(0, 1).flatten(1), k.flatten(0, 1), pos)):
+        got = s4r.qk_norm_rope(c, a, b, p)
+        assert got[0].shape == a.shape and got[1].shape == b.shape
+        assert all(torch.equal(x.flatten(), y.flatten()) for x, y in zip(got, want))
+        got = s4r.qk_norm_rope(c, a, b, p, q_out=out.view(B * N, HQ, DH), k_out=torch.empty_like(k))
+        assert all(torch.equal(x.flatten(), y.flatten()) for x, y in zip(got, want))
