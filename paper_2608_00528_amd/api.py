@@ -644,15 +644,17 @@ def _kv8(cfg, cache, dev):
     """The C view of a cache, its tensors checked against cfg."""
     if not isinstance(cache, KV8Cache):
         raise ValueError("cache must be a KV8Cache")
-    blocks = cfg.batch * cfg.n_kv_heads * ((cfg.capacity + L.KV8_BLOCK - 1) // L.KV8_BLOCK)
-    codes = blocks * L.KV8_BLOCK * cfg.head_dim
+    scales = (cfg.batch, cfg.n_kv_heads, (cfg.capacity + L.KV8_BLOCK - 1) // L.KV8_BLOCK)
+    codes = scales + (L.KV8_BLOCK * cfg.head_dim,)
     kc, ks, vc, vs = cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales
     view = L.KV8(_KV_FORMATS[cache.format], _ptr(kc, "k_codes", torch.uint8), _ptr(ks, "k_scales", torch.float32),
                  _ptr(vc, "v_codes", torch.uint8), _ptr(vs, "v_scales", torch.float32))
-    for name, t, n in (("k_codes", kc, codes), ("k_scales", ks, blocks), ("v_codes", vc, codes),
-                       ("v_scales", vs, blocks)):
-        if t.numel() != n:
-            raise ValueError(f"{name} has {t.numel()} elements, expected {n}")
+    for name, t, shape in (("k_codes", kc, codes), ("k_scales", ks, scales), ("v_codes", vc, codes),
+                           ("v_scales", vs, scales)):
+        if t.shape != shape:
+            if t.numel() != math.prod(shape):
+                raise ValueError(f"{name} has {t.numel()} elements, expected {shape}")
+            _same_order(t.shape, shape, f"{name} and cfg's cache")
         if t.get_device() != dev:
             _here(t, name, dev)
     return ctypes.byref(view)

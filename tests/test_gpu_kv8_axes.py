@@ -112,3 +112,23 @@ def test_heads_of_the_same_tokens():
         assert all(torch.equal(x.flatten(), y.flatten()) for x, y in zip(got, want))
         got = s4r.qk_norm_rope(c, a, b, p, q_out=out.view(B * N, HQ, DH), k_out=torch.empty_like(k))
         assert all(torch.equal(x.flatten(), y.flatten()) for x, y in zip(got, want))
+
+
+def test_cache_of_another_config():
+    """As many elements, other sequences and heads."""
+    c, other = cfg(B, HQ, HKV, DH, CAP), cfg(HKV, HQ, B, DH, CAP)
+    cache, ws = s4r.kv8_alloc(other), s4r.alloc_kv8_workspace(c)
+    x = rand(B, N, HKV, DH)
+    refused(lambda: s4r.kv8_write(c, cache, x, x), "axes")
+    refused(lambda: s4r.kv8_read(c, cache, N), "axes")
+    refused(lambda: s4r.kv8_decode(c, cache, 100, rand(B, HQ, DH), ws), "axes")
+    mine = s4r.kv8_alloc(c)
+    mine.v_scales = cache.v_scales
+    refused(lambda: s4r.kv8_write(c, mine, x, x), "axes")
+    assert not cache.k_codes.any() and not mine.k_codes.any() and not cache.v_scales.any()
+    # flat memory of the program's own
+    mine = s4r.kv8_alloc(c)
+    flat = s4r.KV8Cache("int8", *[t.view(-1) for t in (mine.k_codes, mine.k_scales, mine.v_codes, mine.v_scales)])
+    s4r.kv8_write(c, flat, x, x)
+    assert all(torch.equal(a, b) for a, b in zip(s4r.kv8_read(c, flat, N), s4r.kv8_read(c, mine, N)))
+    assert mine.k_scales.any()
