@@ -412,9 +412,11 @@ s4r_status s4r_dense_decode(const s4r_config* cfg, int64_t N, const void* q, con
  *   q_weight, k_weight [d_h] storage dtype or NULL; eps finite and >= 0.
  *   positions int32 [n_tokens], 4-byte aligned, any values (NULL only when
  *   rope_theta is 0).
- * Sums of squares are fp32, and fp64 for heads whose squares leave its range; the
- * angle is exact to 2^-25 of a revolution for positions below 2^26, to 2^-21 for
- * any; rounded once.  Uses cfg's head counts, head_dim, rope_theta and dtype.
+ * Sums of squares are fp32, and fp64 for heads whose squares leave its range; for
+ * bases of 1 and more the angle is exact to 2^-26 of a revolution at positions below
+ * 2^26 and to 2^-21 at any (below 1 its error grows with the largest frequency,
+ * theta^-1); its sine and cosine are within fp32's rounding of their own size for fp32
+ * rows and within 2^-20 for bf16 ones; rounded once.  Uses cfg's head counts, head_dim, rope_theta and dtype.
  */
 s4r_status s4r_qk_norm_rope(const s4r_config* cfg, int64_t n_tokens, const void* q, int64_t q_stride,
                             const void* k, int64_t k_stride, const void* q_weight, const void* k_weight,

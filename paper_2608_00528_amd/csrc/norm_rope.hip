@@ -80,12 +80,39 @@ __device__ __forceinline__ void norm_far(float (&x)[8], double eps) {
 }
 
 // cos and sin of pos * F revolutions; F a 0.64 fixed-point number, so the fraction
-// of a revolution is exact in 64-bit integer arithmetic for any position
-__device__ __forceinline__ void turn(int32_t pos, uint64_t F, float& c, float& s) {
+// of a revolution is exact in 64-bit integer arithmetic for any position.  bf16 rows take
+// the hardware's functions of its upper 24 bits (off by up to 2^-22, next to a bf16
+// step of 2^-8).  fp32 rows would lose by it what they hold: they take the fraction from the
+// nearest quarter, its first 24 bits wherever they begin, and the functions' series, which on
+// [-pi / 4, pi / 4] end below 2^-28.
+template <typename T>
+__device__ __forceinline__ void turn(int32_t pos, uint64_t F, float& c, float& s);
+template <>
+__device__ __forceinline__ void turn<uint16_t>(int32_t pos, uint64_t F, float& c, float& s) {
   const uint64_t phase = (uint64_t)(int64_t)pos * F;
   const float x = (float)(int32_t)(phase >> 32) * 2.3283064365386963e-10f;   // revolutions in [-1/2, 1/2)
   c = __builtin_amdgcn_cosf(x);
   s = __builtin_amdgcn_sinf(x);
+}
+template <>
+__device__ __forceinline__ void turn<float>(int32_t pos, uint64_t F, float& c, float& s) {
+  constexpr double A = 6.283185307179586, B = A * A;   // the series in revolutions: powers of 2 pi over factorials
+  constexpr float A1 = (float)A, A0 = (float)(A - (double)A1);
+  constexpr float s3 = (float)(-A * B / 6), s5 = (float)(A * B * B / 120), s7 = (float)(-A * B * B * B / 5040),
+                  s9 = (float)(A * B * B * B * B / 362880);
+  constexpr float c2 = (float)(-B / 2), c4 = (float)(B * B / 24), c6 = (float)(-B * B * B / 720),
+                  c8 = (float)(B * B * B * B / 40320), c10 = (float)(-B * B * B * B * B / 3628800);
+  const uint64_t phase = (uint64_t)(int64_t)pos * F, near = phase + (1ull << 61);
+  const uint32_t quarter = (uint32_t)(near >> 62);
+  const int64_t rest = (int64_t)(phase - ((uint64_t)quarter << 62));          // in [-2^61, 2^61)
+  const uint64_t size = rest < 0 ? -rest : rest;
+  const float r = fmaf((float)(uint32_t)size, 0x1p-64f, (float)(uint32_t)(size >> 32) * 0x1p-32f);
+  const float x = rest < 0 ? -r : r, z = x * x;
+  const float sx = fmaf(x, A1, x * fmaf(z, fmaf(z, fmaf(z, fmaf(z, s9, s7), s5), s3), A0));
+  const float cx = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, c10, c8), c6), c4), c2), 1.f);
+  const float u = quarter & 1 ? sx : cx, v = quarter & 1 ? cx : sx;
+  c = (quarter + 1) & 2 ? -u : u;
+  s = quarter & 2 ? -v : v;
 }
 
 template <typename T, int DH>
@@ -139,7 +166,7 @@ __global__ __launch_bounds__(256) void k_qk_norm_rope(const T* q, int64_t q_stri
     if (ratio != 0.0) {
       const int32_t pos = positions[tok];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) turn(pos, F[v], c[v], s[v]);
+      for (int v = 0; v < 4; ++v) turn<T>(pos, F[v], c[v], s[v]);
     }
     for (; g < g1; ++g) {
       float x[8];
