@@ -416,7 +416,8 @@ s4r_status s4r_dense_decode(const s4r_config* cfg, int64_t N, const void* q, con
  * bases of 1 and more the angle is exact to 2^-26 of a revolution at positions below
  * 2^26 and to 2^-21 at any (below 1 its error grows with the largest frequency,
  * theta^-1); its sine and cosine are within fp32's rounding of their own size for fp32
- * rows and within 2^-20 for bf16 ones; rounded once.  Uses cfg's head counts, head_dim, rope_theta and dtype.
+ * rows and within 2^-20 for bf16 ones; rounded once.  Uses cfg's head counts, head_dim,
+ * rope_theta and dtype.
  */
 s4r_status s4r_qk_norm_rope(const s4r_config* cfg, int64_t n_tokens, const void* q, int64_t q_stride,
                             const void* k, int64_t k_stride, const void* q_weight, const void* k_weight,
@@ -460,7 +461,8 @@ s4r_status s4r_kv8_size(const s4r_config* cfg, size_t* code_bytes, size_t* scale
  * at least the width).  Row i of sequence b becomes token first_b + i,
  * first_b = starts[b] (int32 [B] on the device, 4-byte aligned) or row0 where
  * starts is NULL, for i < counts[b] (device, clamped to [0, n_rows]; NULL: all).
- * A sequence whose range does not lie in [0, capacity) is left as it is.
+ * A sequence whose range does not lie in [0, capacity) is left as it is.  Starts are read
+ * on the device, so the call cannot say so: a caller keeps its lengths within the capacity.
  *   A call that starts inside a block keeps the block's earlier tokens: the scale
  * becomes the larger of the present one and the new rows' own, and where it grows
  * the earlier tokens are written anew from the values they stood for (rounded once

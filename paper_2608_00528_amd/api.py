@@ -662,9 +662,9 @@ def _kv8(cfg, cache, dev):
 
 def kv8_write(cfg, cache, k, v, row0=0, starts=None, counts=None):
     """Quantise rows k, v [B, n, h_kv d_h] (or [B, n, h_kv, d_h]; evenly spaced rows; B and n may be one axis) into
-    the cache as tokens
-    starts[b] + i (int32 GPU tensor; row0 + i without it) for i < counts[b] (all without it).  A sequence whose range
-    does not fit is left as it is."""
+    the cache as tokens starts[b] + i (int32 GPU tensor; row0 + i without it) for i < counts[b] (all without it).  A
+    sequence whose range does not fit is left as it is, without an error: the program keeps its lengths below
+    cfg.capacity."""
     dt, heads, dh = storage_dtype(cfg), cfg.n_kv_heads, cfg.head_dim
     dev = _device()
     c = _kv8(cfg, cache, dev)
