@@ -514,7 +514,7 @@ def _tokens(t, heads, dh):
     """The axes of a tensor's rows where they are several."""
     shape = t.shape
     d, n = len(shape), 1
-    if d < 3 or (d == 3 and shape[-1] == dh and shape[-2] == heads):
+    if d < 3 or (d == 3 and shape[-1] == dh):
         return None
     while d and n < heads * dh:
         d -= 1
@@ -540,7 +540,7 @@ def qk_norm_rope(cfg, q, k, positions, q_weight=None, k_weight=None, eps=1e-6, q
         p, rows, stride = _rows(x, name, dt, heads, dh, dev)
         if n is not None and rows != n:
             raise ValueError(f"q has {n} tokens and k {rows}")
-        n, own = rows, _tokens(x, heads, dh)
+        n, own = rows, _tokens(x, heads, dh) if x.dim() > 3 or x.shape[-1] != dh else None
         if own is not None:
             if axes is not None:
                 _same_order(axes, own, "the tokens of q and k")
@@ -644,8 +644,8 @@ def _kv8(cfg, cache, dev):
     """The C view of a cache, its tensors checked against cfg."""
     if not isinstance(cache, KV8Cache):
         raise ValueError("cache must be a KV8Cache")
-    scales = (cfg.batch, cfg.n_kv_heads, (cfg.capacity + L.KV8_BLOCK - 1) // L.KV8_BLOCK)
-    codes = scales + (L.KV8_BLOCK * cfg.head_dim,)
+    batch, heads, tiles = cfg.batch, cfg.n_kv_heads, (cfg.capacity + L.KV8_BLOCK - 1) // L.KV8_BLOCK
+    scales, codes = (batch, heads, tiles), (batch, heads, tiles, L.KV8_BLOCK * cfg.head_dim)
     kc, ks, vc, vs = cache.k_codes, cache.k_scales, cache.v_codes, cache.v_scales
     view = L.KV8(_KV_FORMATS[cache.format], _ptr(kc, "k_codes", torch.uint8), _ptr(ks, "k_scales", torch.float32),
                  _ptr(vc, "v_codes", torch.uint8), _ptr(vs, "v_scales", torch.float32))
@@ -665,18 +665,18 @@ def kv8_write(cfg, cache, k, v, row0=0, starts=None, counts=None):
     the cache as tokens starts[b] + i (int32 GPU tensor; row0 + i without it) for i < counts[b] (all without it).  A
     sequence whose range does not fit is left as it is, without an error: the program keeps its lengths below
     cfg.capacity."""
-    dt, heads, dh = storage_dtype(cfg), cfg.n_kv_heads, cfg.head_dim
+    dt, batch, heads, dh = storage_dtype(cfg), cfg.batch, cfg.n_kv_heads, cfg.head_dim
     dev = _device()
     c = _kv8(cfg, cache, dev)
     pk, rows, sk = _rows(k, "k", dt, heads, dh, dev)
     pv, rv, sv = _rows(v, "v", dt, heads, dh, dev)
-    if rows != rv or rows % cfg.batch:
-        raise ValueError(f"k has {rows} rows and v {rv}: a multiple of the batch {cfg.batch}, the same for both, "
-                         "was expected")
-    _batch_first(k.shape, "k", cfg.batch, heads * dh)
-    _batch_first(v.shape, "v", cfg.batch, heads * dh)
-    L.check(L.load().s4r_kv8_write(_cfgp(cfg), c, rows // cfg.batch, row0, _ints(starts, "starts", cfg.batch, dev),
-                                   _ints(counts, "counts", cfg.batch, dev), pk, sk, pv, sv, _stream()))
+    if rows != rv or rows % batch:
+        raise ValueError(f"k has {rows} rows and v {rv}: a multiple of the batch {batch}, the same for both, was expected")
+    if k.shape[0] != batch or v.shape[0] != batch:
+        _batch_first(k.shape, "k", batch, heads * dh)
+        _batch_first(v.shape, "v", batch, heads * dh)
+    L.check(L.load().s4r_kv8_write(_cfgp(cfg), c, rows // batch, row0, _ints(starts, "starts", batch, dev),
+                                   _ints(counts, "counts", batch, dev), pk, sk, pv, sv, _stream()))
 
 
 def kv8_read(cfg, cache, n_rows, row0=0, starts=None, counts=None, k=None, v=None):
@@ -728,24 +728,26 @@ def kv8_decode(cfg, cache, n_tokens, q, ws, lengths=None, out=None):
     dt = storage_dtype(cfg)
     dev = _device()
     c = _kv8(cfg, cache, dev)
-    per = cfg.batch * cfg.n_q_heads * cfg.head_dim
+    batch, dh = cfg.batch, cfg.head_dim
     p = _ptr(q, "q", dt)
     _here(q, "q", dev)
-    if q.numel() == 0 or q.numel() % per:
-        raise ValueError(f"q has shape {tuple(q.shape)}: [batch, n, n_q_heads, head_dim] was expected")
-    if q.shape[0] != cfg.batch or q.shape[-1] != cfg.head_dim:
+    shape, n = q.shape, q.numel()
+    n_q, left = divmod(n, batch * cfg.n_q_heads * dh)
+    if left or not n_q:
+        raise ValueError(f"q has shape {tuple(shape)}: [batch, n, n_q_heads, head_dim] was expected")
+    if shape[-1] != dh or shape[0] != batch:
         _queries(q, "q", cfg)
     if out is None:
-        out = q.new_empty(q.shape, dtype=torch.float32)
-    elif out.numel() != q.numel():
-        raise ValueError(f"out has {out.numel()} elements, expected {q.numel()}")
-    elif out.shape != q.shape:
+        out = q.new_empty(shape, dtype=torch.float32)
+    elif out.shape != shape:
+        if out.numel() != n:
+            raise ValueError(f"out has {out.numel()} elements, expected {n}")
         _queries(out, "out", cfg)
     po, pw = _ptr(out, "out", torch.float32), _ptr(ws, "ws", torch.uint8)
     _here(out, "out", dev)
     _here(ws, "ws", dev)
-    L.check(L.load().s4r_kv8_decode(_cfgp(cfg), c, n_tokens, _ints(lengths, "lengths", cfg.batch, dev), q.numel() // per, p,
-                                    po, pw, ws.numel(), _stream()))
+    L.check(L.load().s4r_kv8_decode(_cfgp(cfg), c, n_tokens, _ints(lengths, "lengths", batch, dev), n_q, p, po, pw,
+                                    ws.numel(), _stream()))
     return out
 
 
