@@ -9,8 +9,8 @@
 // bytes of codes per block.  The heads of a block run side by side, so the rows' lines
 // are used whole (a head's blocks side by side: 624 us and 816 us), and what passes
 // through once goes past the caches (without: 563 and 583).  4 x 131068 rows of 8 heads
-// of 128, bf16, K and V: written in 523 us (6.2 TB/s), read in 568 us (5.7 TB/s); one
-// row for each of 32 sequences 7.3 us, most of it the chain start -> rows -> scale.
+// of 128, bf16, K and V: written in 520 us (6.2 TB/s), read in 571 us (5.6 TB/s); one
+// row for each of 32 sequences 6.9 us, most of it the chain start -> rows -> scale.
 #include "kv8.h"
 
 namespace s4r {

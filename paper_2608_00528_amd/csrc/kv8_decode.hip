@@ -30,12 +30,13 @@
 // merges them in order.  Lengths are read on the device, so a captured graph follows them.
 // Short caches have a workgroup or, in large batches, a wave for each pair instead.
 //
-// Measured (kernel): 4 x 131068 tokens, 8 KV heads of 128: 155 us, 6.9 TB/s (a large
-// read reaches 6.2, a copy 5.1), 565 VALU and 48 MFMA instructions a block; with two
-// workgroups per CU 165 us, with eight waves per workgroup 164: more reads on their way
-// than 64 KB per CU make the memory slower.  A block takes a wave 2.2 us; 7 us are the
-// launch, the first block's way and the merge (1 x 32764 tokens: 15.8 us for four blocks
-// a wave, and 4 us for k_kv8_combine).
+// Measured (kernel): 4 x 131068 tokens, 8 KV heads of 128: 161 us, 6.7 TB/s (a large
+// read reaches 6.2, a copy 5.1), 621 VALU and 64 MFMA instructions a block of int8 codes, 365
+// and 64 of e4m3.  Workgroups in all, with k_kv8_combine: 128 / 192 / 256 / 320 / 384 / 512
+// take 221 / 167 / 165 / 213 / 181 / 168 us: more reads on their way than 64 KB per CU make
+// the memory no faster.  A block takes a wave 1.6 to 1.8 us of a quiet chip (8 pairs of 512 /
+// 1024 / 2048 tokens, a workgroup each: 7.7 / 10.8 / 17.9 us) and 2.4 at the memory's rate; 1 x
+// 32764 tokens are 17.2 us for four blocks a wave, and 3.9 for k_kv8_combine.
 #include "kv8.h"
 
 namespace s4r {
@@ -110,8 +111,9 @@ __device__ __forceinline__ int wave_scan(int x) {               // inclusive pre
 
 // The (sequence, KV head) pairs lie on a line that is cut into equal runs.  A pair takes
 // its blocks rounded up to one for every wave, and room for another round where it is
-// shorter than a run: ending a pair costs a run about as much (2.4 us), and a run of
-// many short pairs would end long after the others.
+// shorter than a run: ending a pair costs a run about as much, and a run of many short
+// pairs would end long after the others (with / without: 32 sequences of 0 to 32765 tokens 167 /
+// 169 us, 256 of 1 to 1000 69 / 88).
 __host__ __device__ inline int pair_length(int blocks, int shorter) {
   return blocks == 0 ? 0 : (blocks + kWaves - 1) / kWaves * kWaves + (blocks < shorter ? kWaves : 0);
 }
@@ -219,8 +221,8 @@ __device__ __forceinline__ int64_t part_row(int slot, int chunks, int chunk, int
 // their conversion.  SHARE: waves that take a pair's blocks in turn - the workgroup's, or
 // 1: a pair to each wave, nothing to merge, and a workgroup's waves never wait for each
 // other (one_wave_per_pair).  Two workgroups' registers fit a CU but for fp32 queries over
-// 128 dims, whose parts take 264: held to 256, 8 x 16256 tokens of 8 KV heads take 57 us, not
-// 51, and 512 pairs of 512 tokens 21.5, not 20.5
+// 128 dims, whose parts take 264: held to 256, 8 x 16256 tokens of 8 KV heads take 57.0 us,
+// not 51.0, 4 x 131068 of e4m3 171.7, not 165.0, and 512 pairs of 512 21.8, not 20.0
 template <typename T, int FMT, int DH, int RC, int SHARE>
 __global__ __launch_bounds__(kWaves * 64, RC == 1 && (sizeof(T) == 2 || DH == 64) ? 2 : 1) void k_kv8_decode(
     const T* __restrict__ q, const uint8_t* __restrict__ k_codes, const float* __restrict__ k_scales,
@@ -306,7 +308,7 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 && (sizeof(T) == 2 || DH == 64
 
   // Workgroups start a sixteenth of their part of a pair apart and come round to its
   // beginning: in step, with caches a few blocks short of a power of two, their streams
-  // meet on the same memory channels (8 x 16256 tokens, 8 KV heads: 55 us; so 48 us).
+  // meet on the same memory channels (8 x 16256 tokens, 8 KV heads: 57 us; so 50 us).
   // The block of a pair that is read for position p of its part [us, ue):
   auto block_at = [&](const Pair& at, int p, int us, int ue) __attribute__((always_inline)) {
     const int rounds = (ue - us) / SHARE, turned = us + rounds * SHARE;
@@ -594,8 +596,8 @@ __global__ __launch_bounds__(kWaves * 64, RC == 1 && (sizeof(T) == 2 || DH == 64
 // runs), of a run: for the pair that begins in it and goes on behind it.  Groups of DH / 4
 // threads over the partials, each with its own running maximum (one round of loads).
 // Each of them works out the line, so fewer are better: both kernels, a workgroup for every
-// pair / every run: 3000 pairs of 1 to 200 tokens (N 2112) 136 / 62.5 us, 4096 of 64 (N
-// 4096) 107 / 66.9, 1024 of 4000 166.4 / 162.2
+// pair / every run: 3000 pairs of 1 to 200 tokens (N 2112) 135 / 64 us, 4096 of 64 (N
+// 4096) 114 / 74, 1024 of 4000 169.7 / 165.6; 64 of 4000 18.5 / 19.7
 template <int DH>
 __global__ __launch_bounds__(256) void k_kv8_combine(const float* __restrict__ part_ml, const float* __restrict__ part_o,
                                                      float* __restrict__ out, Seqs S, int nwg, int by_cut, int chunks,
@@ -674,14 +676,16 @@ __global__ __launch_bounds__(256) void k_kv8_combine(const float* __restrict__ p
 }
 
 int row_chunks(const Problem& P, int n_q) { return (n_q * P.G + kKv8Rows - 1) / kKv8Rows; }
-// workgroups over the query rows: two chunks each where there are two (five query tokens
-// of four heads over 120001 tokens: 76 us in two workgroups)
+// workgroups over the query rows: two chunks each where there are two (against one each,
+// query tokens of four heads over 120001 tokens: 5 59.8 / 66.9 us, 8 65.5 / 67.7, 12 102.5 / 101.8,
+// 16 103 / 112, 32 179 / 195; fp32 ones, 8 74 / 84, 32 206 / 250)
 int row_sets(const Problem& P, int n_q) { return (row_chunks(P, n_q) + 1) / 2; }
 // a workgroup for each pair where the caches are short: its waves take 4 blocks each at
 // most, 8 where the pairs fill half the chip, and nothing is left to merge.  One launch
-// against two, in a graph: 1024 tokens, 8 pairs 9.6 / 9.2 us (calls from Python 10.0 /
-// 11.8), 128 pairs 10.8 / 13.0; 2048 tokens, 8 pairs 15.4 / 10.0, 128 pairs 16.1 / 17.6,
-// 512 pairs 46.0 / 47.0
+// against two, in a graph: 512 tokens, 8 pairs 7.7 / 9.3 us; 1024 tokens, 8 pairs 10.8 / 9.4
+// (but calls from Python, which pay for each launch, 11.0 / 13.1), 64 pairs 11.6 / 11.2, 128
+// pairs 11.9 / 14.1; 2048 tokens, 8 pairs 17.9 / 10.1, 128 pairs 18.7 / 18.9, 512 pairs
+// 47.6 / 48.7
 bool one_workgroup_per_pair(const Problem& P, int sets, int64_t n_max) {
   const int64_t groups = (int64_t)P.B * P.hkv * sets;
   const int blocks = groups >= 128 ? 8 * kWaves : 4 * kWaves;
@@ -689,12 +693,12 @@ bool one_workgroup_per_pair(const Problem& P, int sets, int64_t n_max) {
 }
 // a wave for each pair where there are enough of them to fill the chip and the caches are
 // shorter still: nothing is merged, and the chip holds 2048 pairs at a time, not 512.  A
-// wave's blocks come one after the other (512 tokens take 18 us), so longer ones only where
-// there are many, or 32 query rows to merge.  In us, a workgroup / a wave per pair: 640
-// pairs of 512 tokens 20.8 / 17.3, 1024 of 200 22.3 / 15.5, of 512 30.9 / 24.8, of 1 to 512
-// 22.0 / 19.3; 2048 of 1024 98.8 / 85.4; 8192 of 64 83.8 / 40.1, of 1024 404 / 355; nine
-// query tokens over 1000, 640 sets of rows 57.3 / 42.0, 2048 154 / 93.5.  The other way: 512
-// pairs of 512 17.1 / 19.3, 1024 of 1 to 2000 52.7 / 57.2, nine query tokens, 512 sets 39.7 / 43.0
+// wave's blocks come one after the other (512 tokens take 20 us), so longer ones only where
+// there are many, or 32 query rows to merge.  Pairs count once for each set of rows.  In us, a
+// workgroup / a wave per pair: 640 pairs of 512 tokens 22.5 / 20.7, 1024 of 200 22.4 / 15.1, of
+// 512 32.1 / 25.4, of 1 to 512 23.0 / 21.0; 2048 of 1024 100 / 87; 8192 of 64 87 / 37, of 1024
+// 411 / 357; nine query tokens over 1000, 1280 sets of rows 105 / 95, 4096 334 / 205.  The other
+// way: 512 pairs of 512 16.6 / 20.1, 1024 of 1 to 2000 53.2 / 62.3
 bool one_wave_per_pair(const Problem& P, int n_q, int64_t n_max) {
   const int64_t groups = (int64_t)P.B * P.hkv * row_sets(P, n_q);
   const int blocks = groups >= 2048 || row_chunks(P, n_q) > 1 ? 16 : 8;

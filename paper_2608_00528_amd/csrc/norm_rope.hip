@@ -216,10 +216,11 @@ hipError_t launch_qk_norm_rope(const Problem& P, int64_t n_tokens, const void* q
   const int hq = q ? P.hq : 0, heads = hq + (k ? P.hkv : 0);
   const int hpw = 512 / P.dh, groups = (heads + hpw - 1) / hpw;
   // few tokens: a wave for each group of heads; many: a token's heads in one wave,
-  // which then works out the token's turns once (32764 tokens of 32 + 8 heads: 131 us,
-  // 5.1 TB/s; waves that take several tokens, 256 to 1536 workgroups in all: 133 to
-  // 160 us; stores through the caches 135 us).  One side / the other: 32 tokens 3.8 / 8.1
-  // us, 512 tokens 6.1 / 8.8, 1000 tokens 10.0 / 9.7, 2000 tokens 16.4 / 11.1
+  // which then works out the token's turns once (32764 tokens of 32 + 8 heads: 124 us,
+  // 5.4 TB/s; waves that take several tokens, 256 / 512 / 1024 / 1536 workgroups in all: 281 /
+  // 175 / 126 / 148 us; stores through the caches 132 us).  One side / the other: 32 tokens 3.2 /
+  // 7.4 us, 512 tokens 5.5 / 8.6, 819 tokens 7.9 / 9.3, 1000 tokens 9.5 / 11.2, 2000 tokens
+  // 17.4 / 14.3
   const int per = n_tokens * groups <= 8192 ? 1 : groups;
   const int64_t units = n_tokens * ((groups + per - 1) / per);
   const dim3 grid((unsigned)std::min<int64_t>((units + 3) / 4, 1 << 20));

@@ -116,7 +116,7 @@ inline double rope_ratio(const Problem& P) { return P.theta == 0.f ? 0.0 : pow((
 
 // ---- the 8-bit KV cache ----------------------------------------------------
 constexpr int kKv8Block = 64;         // tokens per block (one scale per side and KV head)
-constexpr int kKv8Rows = 16;          // query rows (query token x group member) per attention workgroup
+constexpr int kKv8Rows = 16;          // query rows (query token x group member) of a chunk, one side of an MFMA
 constexpr int kKv8MaxRows = 128;      // n_q * G
 constexpr int kKv8Wgs = 256;          // attention workgroups: one per CU
 struct Kv8 {
