@@ -418,6 +418,22 @@ def _here(t, name, dev):
         raise ValueError(f"{name} is on {t.device}, not on the current device {dev}")
 
 
+def _same_order(a, b, names):
+    """Axes a and b of as many elements count them in the same order: they are equal, or one's are the other's with
+    some of them as one."""
+    if a == b:
+        return
+    ends = []
+    for shape in (a, b):
+        n, e = 1, {1}
+        for x in shape:
+            n *= x
+            e.add(n)
+        ends.append(e)
+    if not (ends[0] <= ends[1] or ends[1] <= ends[0]):
+        raise ValueError(f"{names} have axes {tuple(a)} and {tuple(b)}")
+
+
 def _batch_first(shape, name, batch, width):
     """The rows of `width` elements in `shape` come sequence by sequence: leading axes that make up the batch, or
     rows in one axis (sequence b's before b + 1's)."""
@@ -492,22 +508,6 @@ def _ints(t, name, n, dev):
     if t.numel() != n:
         raise ValueError(f"{name} has {t.numel()} entries, expected {n}")
     return p
-
-
-def _same_order(a, b, names):
-    """Axes a and b of as many elements count them in the same order: they are equal, or one's are the other's with
-    some of them as one."""
-    if a == b:
-        return
-    ends = []
-    for shape in (a, b):
-        n, e = 1, {1}
-        for x in shape:
-            n *= x
-            e.add(n)
-        ends.append(e)
-    if not (ends[0] <= ends[1] or ends[1] <= ends[0]):
-        raise ValueError(f"{names} have axes {tuple(a)} and {tuple(b)}")
 
 
 def _tokens(t, heads, dh):
@@ -693,8 +693,7 @@ def kv8_read(cfg, cache, n_rows, row0=0, starts=None, counts=None, k=None, v=Non
         elif t.numel() != shape[0] * shape[1] * shape[2]:
             raise ValueError(f"{name} has {t.numel()} elements, expected {shape}")
         elif t.shape != shape:
-            _heads_last(t.shape, name, cfg.n_kv_heads, cfg.head_dim)
-            _batch_first(t.shape, name, cfg.batch, shape[2])
+            _same_order(t.shape, shape[:2] + (cfg.n_kv_heads, cfg.head_dim), f"{name} and the rows")
         out.append(t)
     ptrs = [_ptr(t, name, dt) for t, name in zip(out, "kv")]
     for t, name in zip(out, "kv"):
@@ -714,12 +713,6 @@ def alloc_kv8_workspace(cfg, n_queries=1, device="cuda"):
     return torch.empty(kv8_workspace_size(cfg, n_queries), dtype=torch.uint8, device=device)
 
 
-def _queries(t, name, cfg):
-    """Query tokens of every sequence, [B, n, h_q, d_h] or the same with some of these axes as one."""
-    _heads_last(t.shape, name, cfg.n_q_heads, cfg.head_dim)
-    _batch_first(t.shape, name, cfg.batch, cfg.n_q_heads * cfg.head_dim)
-
-
 def kv8_decode(cfg, cache, n_tokens, q, ws, lengths=None, out=None):
     """Attention of the newest query tokens q [B, h_q, d_h] or [B, n, h_q, d_h] (rotated as the cached keys are)
     over the 8-bit cache: tokens 0 .. n_tokens - 1 of every sequence, or of lengths[b] (int32 GPU tensor, at most
@@ -728,21 +721,22 @@ def kv8_decode(cfg, cache, n_tokens, q, ws, lengths=None, out=None):
     dt = storage_dtype(cfg)
     dev = _device()
     c = _kv8(cfg, cache, dev)
-    batch, dh = cfg.batch, cfg.head_dim
+    batch, hq, dh = cfg.batch, cfg.n_q_heads, cfg.head_dim
     p = _ptr(q, "q", dt)
     _here(q, "q", dev)
     shape, n = q.shape, q.numel()
-    n_q, left = divmod(n, batch * cfg.n_q_heads * dh)
+    n_q, left = divmod(n, batch * hq * dh)
     if left or not n_q:
         raise ValueError(f"q has shape {tuple(shape)}: [batch, n, n_q_heads, head_dim] was expected")
-    if shape[-1] != dh or shape[0] != batch:
-        _queries(q, "q", cfg)
+    order = (batch, n_q, hq, dh)
+    if shape != order and (n_q > 1 or shape != (batch, hq, dh)):
+        _same_order(shape, order, "q and the query tokens")
     if out is None:
         out = q.new_empty(shape, dtype=torch.float32)
     elif out.shape != shape:
         if out.numel() != n:
             raise ValueError(f"out has {out.numel()} elements, expected {n}")
-        _queries(out, "out", cfg)
+        _same_order(out.shape, order, "out and the query tokens")
     po, pw = _ptr(out, "out", torch.float32), _ptr(ws, "ws", torch.uint8)
     _here(out, "out", dev)
     _here(ws, "ws", dev)

@@ -52,11 +52,11 @@ def test_query_tokens_sequence_by_sequence():
     q = rand(B, N, HQ, DH)
     want = s4r.kv8_decode(c, cache, 100, q, ws)
     turned = q.transpose(0, 1).contiguous()
-    refused(lambda: s4r.kv8_decode(c, cache, 100, turned, ws), "sequences")
-    refused(lambda: s4r.kv8_decode(c, cache, 100, q.transpose(2, 3).contiguous(), ws), "expected")
+    refused(lambda: s4r.kv8_decode(c, cache, 100, turned, ws), "axes")
+    refused(lambda: s4r.kv8_decode(c, cache, 100, q.transpose(2, 3).contiguous(), ws), "axes")
     out = torch.full((N, B, HQ, DH), 7.0, device="cuda")
-    refused(lambda: s4r.kv8_decode(c, cache, 100, q, ws, out=out), "sequences")
-    refused(lambda: s4r.kv8_decode(c, cache, 100, q, ws, out=out.view(B, N, DH, HQ)), "expected")
+    refused(lambda: s4r.kv8_decode(c, cache, 100, q, ws, out=out), "axes")
+    refused(lambda: s4r.kv8_decode(c, cache, 100, q, ws, out=out.view(B, N, DH, HQ)), "axes")
     assert bool((out == 7).all())
     # the same rows in other axes
     for shape in ((B * N, HQ, DH), (B, N * HQ, DH), (B, N, HQ * DH), (B, N, HKV, HQ // HKV, DH), (B * N * HQ * DH,)):
@@ -79,8 +79,8 @@ def test_rows_read_into_two_tensors_sequence_by_sequence():
     n = k.numel()
     refused(lambda: s4r.kv8_read(c, cache, N, k=flat[:n], v=flat[n - 8:2 * n - 8]), "overlap")
     refused(lambda: s4r.kv8_read(c, cache, N, k=flat[n - 8:2 * n - 8], v=flat[:n]), "overlap")
-    refused(lambda: s4r.kv8_read(c, cache, N, k=a[0].view(N, B, HKV * DH)), "sequences")
-    refused(lambda: s4r.kv8_read(c, cache, N, v=a[0].view(B, N, DH, HKV)), "expected")
+    refused(lambda: s4r.kv8_read(c, cache, N, k=a[0].view(N, B, HKV * DH)), "axes")
+    refused(lambda: s4r.kv8_read(c, cache, N, v=a[0].view(B, N, DH, HKV)), "axes")
     assert not a.any()
     # side by side, and the same rows in other axes
     s4r.kv8_read(c, cache, N, k=a[1], v=a[0])
@@ -132,3 +132,20 @@ def test_cache_of_another_config():
     s4r.kv8_write(c, flat, x, x)
     assert all(torch.equal(a, b) for a, b in zip(s4r.kv8_read(c, flat, N), s4r.kv8_read(c, mine, N)))
     assert mine.k_scales.any()
+
+
+@pytest.mark.parametrize("n", [2, 5])
+def test_heads_before_tokens_are_refused(n):
+    """[B, heads, n, d_h], the order in which other attention calls take them."""
+    c = cfg(B, HQ, HKV, DH, CAP)
+    plain = s4r.make_config(batch=1, n_q_heads=HQ, n_kv_heads=HKV, head_dim=DH, rank=32, capacity=64)
+    cache, ws = s4r.kv8_alloc(c), s4r.alloc_kv8_workspace(c, n)
+    q, k = rand(B, HQ, n, DH), rand(B, HKV, n, DH)
+    refused(lambda: s4r.kv8_write(c, cache, k, k), "expected")
+    refused(lambda: s4r.kv8_decode(c, cache, 100, q, ws), "axes")
+    out = torch.zeros(B, HQ, n, DH, device="cuda")
+    refused(lambda: s4r.kv8_decode(c, cache, 100, q.transpose(1, 2).contiguous(), ws, out=out), "axes")
+    refused(lambda: s4r.kv8_read(c, cache, n, k=k.zero_()), "axes")
+    refused(lambda: s4r.qk_norm_rope(plain, q, None, None), "expected|spaced")
+    assert not cache.k_codes.any() and not out.any() and not k.any()
+    s4r.kv8_write(c, cache, k.transpose(1, 2).contiguous(), k.transpose(1, 2).contiguous())
